@@ -515,6 +515,88 @@ int hlq_conv2d_backward(const void *G, const void *X, const void *Wt, const hlq_
                         uint64_t seed, int dtype, int flags, void *dX, void *dW, void *workspace,
                         size_t workspace_bytes, void *stream);
 
+/* ---- the operators around the products -------------------------------------------------------- */
+
+/*
+ * What a training step has beside the layers above: group normalisation with its activation, dropout with the residual, and
+ * attention maps with a learned relative position bias.  Further conventions of these calls:
+ *   - tensors need only the alignment of their elements; parameters have an element type of their own (param_dtype,
+ *     table_dtype: HLQ_BF16 or HLQ_F32); arithmetic and sums are fp32, rounded once where a result is stored;
+ *   - a tensor without elements is no error: nothing is enqueued but zeros for parameter gradients that were asked for.
+ *
+ * Dropout.  p in [0, 1] (HLQ_ERR_SHAPE otherwise, NaN included) is rounded to t / 65536, t = floor(65536 p + 1/2); an element is
+ * dropped where its 16 bits of the seeded stream are below t, and becomes 0 whatever it was; what is kept is multiplied by
+ * 65536 / (65536 - t).  Element i takes half i & 1 (the low one first) of word i >> 1 of stream number 4 of `seed`, the streams
+ * being those of the quantisers; i is the element's place in the dense tensor, in an attention map row * Kp + key with Kp = K
+ * rounded up to a multiple of 8.  The mask is stored nowhere: the backward call is given the forward call's p and seed.  With p >
+ * 0 a call takes at most 2^33 elements (HLQ_ERR_SHAPE).
+ */
+
+/*
+ * Y = residual + dropout(X) over n elements (residual NULL: dropout(X)).  The backward pass is this call on the gradient without
+ * a residual.  Y may be X or residual.
+ */
+int hlq_dropout(const void *X, const void *residual, int64_t n, double p, uint64_t seed, int dtype, void *Y, void *stream);
+
+/*
+ * Y = dropout(act(GroupNorm(X) weight + bias)) for channels-last X, Y [Nb, P, C] (P positions, H W of an image): mean and variance
+ * (divided by the count) over the P positions and C / groups consecutive channels of each group, eps > 0 added to the variance.
+ *   weight, bias  [C] of param_dtype, or NULL (ones, zeros)
+ *   mean, rstd    [Nb, groups] fp32, for the backward call, or NULL
+ *   workspace     >= hlq_group_norm_workspace_bytes(..., 0) bytes, 256-byte aligned (it may be 0: then none is used), or NULL for the
+ *                 registered or library-owned one.
+ * HLQ_ERR_SHAPE: P < 1, C % groups, an unknown act, eps not positive, Nb C >= 2^31, C > 2^24, or C / groups too large: up to 1024 is
+ * taken always, and up to 2048 where it is a multiple of 8.
+ */
+#define HLQ_ACT_NONE 0
+#define HLQ_ACT_RELU 1
+#define HLQ_ACT_SILU 2
+#define HLQ_ACT_GELU 3 /* z Phi(z), Phi by the error function */
+size_t hlq_group_norm_workspace_bytes(int64_t Nb, int64_t P, int64_t C, int64_t groups, int dtype, int backward);
+int hlq_group_norm_act(const void *X, const void *weight, const void *bias, int64_t Nb, int64_t P, int64_t C, int64_t groups, float eps, int act,
+                       double p, uint64_t seed, int dtype, int param_dtype, void *Y, float *mean, float *rstd, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradients from dY, X and the forward call's mean and rstd: dX like X, dweight and dbias [C] of param_dtype; each may be
+ * NULL, not all.  The activation's input is computed anew, nothing else is kept.  relu'(0) = 0.
+ *   workspace  >= hlq_group_norm_workspace_bytes(..., 1) bytes, as above.
+ */
+int hlq_group_norm_act_backward(const void *dY, const void *X, const void *weight, const void *bias, const float *mean, const float *rstd,
+                                int64_t Nb, int64_t P, int64_t C, int64_t groups, int act, double p, uint64_t seed, int dtype, int param_dtype,
+                                void *dX, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention map with a learned relative position bias:  for scores S [B, H, Q, K] (products of queries and keys, unscaled)
+ *   z[b,h,q,k] = scale S[b,h,q,k] + table[buckets[rel(q, k)], h];   Pm = dropout(softmax of z over the keys that q sees)
+ * Relative positions: on a sequence (grid_w = 0) rel(q, k) = k - q + Q - 1, of Q + K - 1; on a grid of width grid_w in row order
+ * (Q = K, K % grid_w = 0, height h = K / grid_w) rel = (ky - qy + h - 1) (2 grid_w - 1) + kx - qx + grid_w - 1, of
+ * (2 h - 1) (2 grid_w - 1).
+ *   table    [n_buckets, H] of table_dtype
+ *   buckets  one int32 for every relative position; one outside [0, n_buckets) has no bias (and no gradient)
+ *   mask     NULL (mask_batches = mask_rows = 0), or bytes [mask_batches, mask_rows, K], nonzero where a query sees a key: batch b
+ *            uses mask b % mask_batches; mask_rows is Q, or 1 for all queries alike
+ *   causal   1: query q sees keys up to q + K - Q (the last query sees the last key)
+ * What is not seen is 0 in Pm and in dS whatever S and dP hold there; so is a score of minus infinity, and a row that sees nothing.
+ * HLQ_ERR_SHAPE: K > 16384 (on a grid 4096), H > 65535, a negative size, n_buckets < 1, a grid that does not fit, mask sizes that do not.
+ */
+typedef struct hlq_rel_geom {
+    int32_t B, H, Q, K;
+    int32_t grid_w, n_buckets, causal, mask_batches, mask_rows;
+} hlq_rel_geom;
+int hlq_rel_softmax(const void *S, const void *table, const int32_t *buckets, const uint8_t *mask, const hlq_rel_geom *g, float scale, double p,
+                    uint64_t seed, int dtype, int table_dtype, void *Pm, void *stream);
+
+/*
+ * Its gradients: dS [B, H, Q, K] of the scores, dtable [n_buckets, H] of the table (NULL: not wanted), from dP and the forward
+ * call's inputs; the map is computed anew.
+ *   workspace  >= hlq_rel_softmax_workspace_bytes(...) bytes, 256-byte aligned, or NULL for the registered or library-owned one.
+ */
+size_t hlq_rel_softmax_workspace_bytes(const hlq_rel_geom *g, int dtype);
+int hlq_rel_softmax_backward(const void *dP, const void *S, const void *table, const int32_t *buckets, const uint8_t *mask, const hlq_rel_geom *g,
+                             float scale, double p, uint64_t seed, int dtype, int table_dtype, void *dS, void *dtable, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,11 +2,14 @@
 activation compression at forward time (ACBP), both gradients from the C-ABI library.
 
 This module only routes tensors: the forward product is torch's, everything of the backward pass
-runs in the HIP kernels behind ``binding``.  Nothing here is needed by the library itself.
+runs in the HIP kernels behind ``binding``, and so do both directions of the operators around the products
+(group normalisation with activation and dropout, dropout with a residual, attention maps with a relative
+position bias).  Nothing here is needed by the library itself.
 """
 from __future__ import annotations
 
 import itertools
+import math
 
 import torch
 
@@ -194,3 +197,196 @@ class HlqConv2d(torch.nn.Module):
         self.calls += 1
         return HlqConv2dFunction.apply(x, self.weight, self.stride, self.padding, self.dilation, self.B, self.r,
                                        self.seed + self.calls, self.flags)
+
+
+def _in_memory_order(t):
+    """A dense view of t in the order of its memory -- channels-last images as [Nb, H, W, C] -- and whether it was permuted."""
+    if not t.is_contiguous() and t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last):
+        return t.permute(0, 2, 3, 1), True
+    return t.contiguous(), False
+
+
+class HlqDropoutFunction(torch.autograd.Function):
+    """residual + dropout(x) (residual None: dropout(x)), bf16 or fp32 on the GPU; nothing is kept for the backward pass but p
+    and the seed.  Which elements drop goes by their place in memory: a channels-last image is taken in its own order."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p, seed):
+        xd, ctx.permuted = _in_memory_order(x)
+        rd = None
+        if residual is not None:
+            if residual.shape != x.shape or residual.dtype != x.dtype:
+                raise ValueError("residual must be %s %s like x" % (x.dtype, tuple(x.shape)))
+            rd = (residual.permute(0, 2, 3, 1) if ctx.permuted else residual).contiguous()
+        y = torch.empty_like(xd)
+        hlq.hlq_dropout(xd, rd, p, seed, y)
+        ctx.meta = (p, seed)
+        return y.permute(0, 3, 1, 2) if ctx.permuted else y
+
+    @staticmethod
+    def backward(ctx, gy):
+        dx = None
+        if ctx.needs_input_grad[0]:
+            g = (gy.permute(0, 2, 3, 1) if ctx.permuted else gy).contiguous()
+            dx = torch.empty_like(g)
+            hlq.hlq_dropout(g, None, *ctx.meta, dx)
+            dx = dx.permute(0, 3, 1, 2) if ctx.permuted else dx
+        return dx, gy if ctx.needs_input_grad[1] else None, None, None
+
+
+class HlqDropout(torch.nn.Module):
+    """Dropout, with a residual added where one is given; a fresh seed per call, nothing dropped in eval mode."""
+
+    def __init__(self, p=0.1, seed=0):
+        super().__init__()
+        self.p, self.seed, self.calls = p, _layer_seed(seed), 0
+
+    def forward(self, x, residual=None):
+        if not self.training or self.p == 0.0:
+            return x if residual is None else x + residual
+        self.calls += 1
+        return HlqDropoutFunction.apply(x, residual, self.p, self.seed + self.calls)
+
+
+class HlqGroupNormActFunction(torch.autograd.Function):
+    """dropout(act(group_norm(x) weight + bias)) of x [Nb, C, H, W] in torch's channels_last memory format (others are
+    converted), bf16 or fp32 on the GPU; weight and bias [C] of either type, or None.  Kept for the backward pass: x, which the
+    layer before kept anyway or can free, and two floats a group."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, eps=1e-5, act=hlq.HLQ_ACT_NONE, p=0.0, seed=0):
+        x_l = x.permute(0, 2, 3, 1).contiguous()         # a view when x is channels_last
+        Nb, H, W, Cc = x_l.shape
+        y = torch.empty_like(x_l)
+        mean, rstd = (torch.empty((Nb, groups), dtype=torch.float32, device=x.device) for _ in range(2))
+        need = hlq.hlq_group_norm_workspace_bytes(Nb, H * W, Cc, groups, x.dtype)
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        hlq.hlq_group_norm_act(x_l, weight, bias, groups, eps, act, y, mean, rstd, ws, p, seed)
+        ctx.save_for_backward(x_l, weight, bias, mean, rstd)
+        ctx.meta = (groups, act, p, seed)
+        return y.permute(0, 3, 1, 2)
+
+    @staticmethod
+    def backward(ctx, gy):
+        x_l, weight, bias, mean, rstd = ctx.saved_tensors
+        groups, act, p, seed = ctx.meta
+        g = gy.permute(0, 2, 3, 1).contiguous()
+        if g.dtype != x_l.dtype:
+            raise TypeError("gradient must be %s like the input, got %s" % (x_l.dtype, g.dtype))
+        dx = torch.empty_like(x_l) if ctx.needs_input_grad[0] else None
+        dw = torch.empty_like(weight) if ctx.needs_input_grad[1] else None
+        db = torch.empty_like(bias) if ctx.needs_input_grad[2] else None
+        if dx is not None or dw is not None or db is not None:
+            Nb, H, W, Cc = x_l.shape
+            need = hlq.hlq_group_norm_workspace_bytes(Nb, H * W, Cc, groups, x_l.dtype, True)
+            ws = torch.empty(need, dtype=torch.uint8, device=g.device) if need else None
+            hlq.hlq_group_norm_act_backward(g, x_l, weight, bias, mean, rstd, groups, act, dx, dw, db, ws, p, seed)
+        return None if dx is None else dx.permute(0, 3, 1, 2), dw, db, None, None, None, None, None
+
+
+_ACTS = {None: hlq.HLQ_ACT_NONE, "none": hlq.HLQ_ACT_NONE, "relu": hlq.HLQ_ACT_RELU, "silu": hlq.HLQ_ACT_SILU, "gelu": hlq.HLQ_ACT_GELU}
+
+
+class HlqGroupNormAct(torch.nn.Module):
+    """Group normalisation with a learned scale and shift, an activation (None, "relu", "silu", "gelu") and dropout in one pass,
+    for channels-last images [Nb, C, H, W]; a fresh seed per call, nothing dropped in eval mode."""
+
+    def __init__(self, groups, channels, act=None, p=0.0, eps=1e-5, dtype=torch.float32, device="cuda", seed=0):
+        super().__init__()
+        if channels % groups:
+            raise ValueError("%d channels are no whole groups of %d" % (channels, groups))
+        self.weight = torch.nn.Parameter(torch.ones(channels, dtype=dtype, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, dtype=dtype, device=device))
+        self.groups, self.act, self.eps, self.p = groups, _ACTS[act], eps, p
+        self.seed, self.calls = _layer_seed(seed), 0
+
+    def forward(self, x):
+        self.calls += 1
+        return HlqGroupNormActFunction.apply(x, self.weight, self.bias, self.groups, self.eps, self.act,
+                                             self.p if self.training else 0.0, self.seed + self.calls)
+
+
+class HlqRelSoftmaxFunction(torch.autograd.Function):
+    """dropout(softmax(scale s + bias)) over the keys of s [B, H, Q, K] with the bias of hlq_rel_softmax: table [n_buckets, H],
+    buckets [relative positions] int32, mask bytes [mask_batches, 1 or Q, K] or None.  s is kept for the backward pass, the map
+    is computed anew there."""
+
+    @staticmethod
+    def forward(ctx, s, table, buckets, mask=None, grid_w=0, causal=False, scale=1.0, p=0.0, seed=0):
+        s_d = s.contiguous()
+        B, H, Q, K = s_d.shape
+        mask = None if mask is None else mask.contiguous()
+        geom = hlq.hlq_rel_geom(B=B, H=H, Q=Q, K=K, grid_w=grid_w, n_buckets=table.shape[0], causal=int(bool(causal)),
+                                mask_batches=0 if mask is None else mask.shape[0], mask_rows=0 if mask is None else mask.shape[1])
+        table_d = table.contiguous()
+        y = torch.empty_like(s_d)
+        hlq.hlq_rel_softmax(s_d, table_d, buckets, mask, geom, scale, y, p, seed)
+        ctx.save_for_backward(s_d, table_d, buckets, mask)
+        ctx.meta = (geom, scale, p, seed)
+        return y
+
+    @staticmethod
+    def backward(ctx, gy):
+        s, table, buckets, mask = ctx.saved_tensors
+        geom, scale, p, seed = ctx.meta
+        ds = dt = None
+        if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
+            ds = torch.empty_like(s)
+            dt = torch.empty_like(table) if ctx.needs_input_grad[1] else None
+            need = hlq.hlq_rel_softmax_workspace_bytes(geom, s.dtype)
+            ws = torch.empty(need, dtype=torch.uint8, device=s.device) if need else None
+            hlq.hlq_rel_softmax_backward(gy.contiguous(), s, table, buckets, mask, geom, scale, ds, dt, ws, p, seed)
+        return (ds if ctx.needs_input_grad[0] else None), dt, None, None, None, None, None, None, None
+
+
+def grid_buckets(height, width, signed=True):
+    """(buckets int32 [(2 height - 1)(2 width - 1)], their number) of the relative positions on a grid: one for each pair of signed
+    distances, or of absolute ones."""
+    dy = torch.arange(1 - height, height)[:, None].expand(2 * height - 1, 2 * width - 1)
+    dx = torch.arange(1 - width, width)[None, :].expand(2 * height - 1, 2 * width - 1)
+    if signed:
+        n = (2 * height - 1) * (2 * width - 1)
+        return torch.arange(n, dtype=torch.int32), n
+    return (dy.abs() * width + dx.abs()).reshape(-1).to(torch.int32), height * width
+
+
+def sequence_buckets(Q, K, n_buckets, max_distance=128, causal=True):
+    """(buckets int32 [Q + K - 1], n_buckets) of the distances on a sequence whose last query is its last key: near distances one
+    bucket each, far ones over their logarithm up to max_distance, the rest in the last.  Not causal: half of the buckets are for keys
+    ahead of the query."""
+    ahead = torch.arange(Q + K - 1) - (K - 1)             # key minus query, queries counted from key K - Q
+    n = n_buckets if causal else n_buckets // 2
+    d = (-ahead).clamp(min=0) if causal else ahead.abs()
+    exact = max(1, n // 2)
+    far = exact + (torch.log(d.clamp(min=1).double() / exact) / math.log(max(max_distance, exact + 1) / exact) * (n - exact)).long()
+    b = torch.where(d < exact, d, far.clamp(max=n - 1))
+    if not causal:
+        b = b + n * (ahead > 0)
+    return b.to(torch.int32), n_buckets
+
+
+class HlqRelSoftmax(torch.nn.Module):
+    """Attention map of scores [B, heads, Q, K] with a learned bias per head and bucket of relative positions, and dropout; a fresh
+    seed per call, nothing dropped in eval mode.
+
+    grid = (height, width): tokens on a grid in row order, buckets of signed or absolute distances.  Without a grid: a
+    sequence, ``n_buckets`` of distances; any Q and K (the buckets of the latest lengths are kept)."""
+
+    def __init__(self, heads, grid=None, signed=True, n_buckets=32, max_distance=128, causal=False, scale=1.0, p=0.0,
+                 dtype=torch.float32, device="cuda", seed=0):
+        super().__init__()
+        self.grid, self.causal, self.scale, self.p, self.max_distance = grid, causal, scale, p, max_distance
+        self.lengths = None
+        if grid is not None:
+            of, n_buckets = grid_buckets(*grid, signed=signed)
+            self.register_buffer("buckets", of.to(device), persistent=False)
+        self.table = torch.nn.Parameter(torch.randn((n_buckets, heads), dtype=torch.float32, device=device).mul_(0.02).to(dtype))
+        self.seed, self.calls = _layer_seed(seed), 0
+
+    def forward(self, s, mask=None):
+        if self.grid is None and self.lengths != (s.shape[2], s.shape[3], s.device):
+            of, _ = sequence_buckets(s.shape[2], s.shape[3], self.table.shape[0], self.max_distance, self.causal)
+            self.buckets, self.lengths = of.to(s.device), (s.shape[2], s.shape[3], s.device)
+        self.calls += 1
+        return HlqRelSoftmaxFunction.apply(s, self.table, self.buckets, mask, self.grid[1] if self.grid else 0, self.causal, self.scale,
+                                           self.p if self.training else 0.0, self.seed + self.calls)

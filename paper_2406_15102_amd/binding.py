@@ -35,7 +35,14 @@ class hlq_conv_geom(C.Structure):
                                            "pad_w", "dil_h", "dil_w")]
 
 
+class hlq_rel_geom(C.Structure):
+    """Geometry of an attention map with a relative position bias, field for field the C struct of the same name."""
+    _fields_ = [(n, C.c_int32) for n in ("B", "H", "Q", "K", "grid_w", "n_buckets", "causal", "mask_batches", "mask_rows")]
+
+
 _GEOM_P = C.POINTER(hlq_conv_geom)
+_REL_P = C.POINTER(hlq_rel_geom)
+HLQ_ACT_NONE, HLQ_ACT_RELU, HLQ_ACT_SILU, HLQ_ACT_GELU = 0, 1, 2, 3
 
 _EXPORTS = {
     "hlq_status_str": (C.c_char_p, [C.c_int]),
@@ -98,6 +105,16 @@ _EXPORTS = {
     "hlq_conv_workspace_bytes": (C.c_size_t, [_GEOM_P, C.c_int, C.c_int, C.c_int, C.c_int]),
     "hlq_conv2d_backward": (C.c_int, [C.c_void_p] * 3 + [_GEOM_P, C.c_int, C.c_int, C.c_uint64, C.c_int, C.c_int]
                             + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]),
+    "hlq_dropout": (C.c_int, [C.c_void_p] * 2 + [C.c_int64, C.c_double, C.c_uint64, C.c_int, C.c_void_p, C.c_void_p]),
+    "hlq_group_norm_workspace_bytes": (C.c_size_t, [C.c_int64] * 4 + [C.c_int] * 2),
+    "hlq_group_norm_act": (C.c_int, [C.c_void_p] * 3 + [C.c_int64] * 4 + [C.c_float, C.c_int, C.c_double, C.c_uint64, C.c_int, C.c_int]
+                           + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]),
+    "hlq_group_norm_act_backward": (C.c_int, [C.c_void_p] * 6 + [C.c_int64] * 4 + [C.c_int, C.c_double, C.c_uint64, C.c_int, C.c_int]
+                                    + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]),
+    "hlq_rel_softmax": (C.c_int, [C.c_void_p] * 4 + [_REL_P, C.c_float, C.c_double, C.c_uint64, C.c_int, C.c_int] + [C.c_void_p] * 2),
+    "hlq_rel_softmax_workspace_bytes": (C.c_size_t, [_REL_P, C.c_int]),
+    "hlq_rel_softmax_backward": (C.c_int, [C.c_void_p] * 5 + [_REL_P, C.c_float, C.c_double, C.c_uint64, C.c_int, C.c_int]
+                                 + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]),
 }
 
 _lib = None
@@ -476,3 +493,119 @@ def hlq_backward_products(Gq, sG, WqT, sW, gx_bits, GhatT, sGhat, XhatT, sXhat, 
                                        gx_bits, _ptr(GhatT), _ptr(sGhat, torch.float32), _ptr(XhatT),
                                        _ptr(sXhat, torch.float32), N, d_in, d_out, Kc, B, _dt(dX), _ptr(dX), _ptr(dW),
                                        ws_ptr, ws_bytes, _stream()), "hlq_backward_products")
+
+
+# ---- the operators around the products ----
+
+def _dtype_code(dtype):
+    if dtype == torch.bfloat16:
+        return HLQ_BF16
+    if dtype == torch.float32:
+        return HLQ_F32
+    raise TypeError("element type must be bfloat16 or float32, got %s" % dtype)
+
+
+def _expect_like(name, t, like):
+    if t is not None and (t.dtype != like.dtype or t.shape != like.shape):
+        raise ValueError("%s must be %s %s like the input, got %s %s" % (name, like.dtype, tuple(like.shape), t.dtype, tuple(t.shape)))
+
+
+def _expect_vector(name, t, shape, dtype):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+        raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
+
+
+def hlq_dropout(X, residual, p, seed, Y):
+    """Y <- residual + dropout(X) (residual None: dropout(X)); the backward pass is the same call on the gradient."""
+    _expect_like("residual", residual, X)
+    _expect_like("Y", Y, X)
+    _check(lib().hlq_dropout(_ptr(X), _ptr(residual), X.numel(), p, seed, _dt(X), _ptr(Y), _stream()), "hlq_dropout")
+
+
+def hlq_group_norm_workspace_bytes(Nb, P, C_, groups, dtype, backward=False) -> int:
+    return int(lib().hlq_group_norm_workspace_bytes(Nb, P, C_, groups, _dtype_code(dtype), int(bool(backward))))
+
+
+def _group_norm_sizes(X, weight, bias, groups):
+    """(Nb, P, C, element type of the parameters) of channels-last X [Nb, ..., C]"""
+    if X.dim() < 2:
+        raise ValueError("X must be [Nb, ..., C], got %s" % (tuple(X.shape),))
+    Nb, C_ = X.shape[0], X.shape[-1]
+    P = 1
+    for d in X.shape[1:-1]:
+        P *= d
+    params = weight if weight is not None else bias
+    pdt = torch.float32 if params is None else params.dtype
+    _expect_vector("weight", weight, (C_,), pdt)
+    _expect_vector("bias", bias, (C_,), pdt)
+    return Nb, P, C_, pdt
+
+
+def hlq_group_norm_act(X, weight, bias, groups, eps, act, Y, mean=None, rstd=None, workspace=None, p=0.0, seed=0):
+    """Y <- dropout(act(GroupNorm(X) weight + bias)) of channels-last X [Nb, ..., C]; mean, rstd [Nb, groups] fp32 for the backward call."""
+    Nb, P, C_, pdt = _group_norm_sizes(X, weight, bias, groups)
+    _expect_like("Y", Y, X)
+    _expect_vector("mean", mean, (Nb, groups), torch.float32)
+    _expect_vector("rstd", rstd, (Nb, groups), torch.float32)
+    wp, wb = _ws(workspace)
+    _check(lib().hlq_group_norm_act(_ptr(X), _ptr(weight), _ptr(bias), Nb, P, C_, groups, eps, act, p, seed, _dt(X), _dtype_code(pdt),
+                                    _ptr(Y), _ptr(mean), _ptr(rstd), wp, wb, _stream()), "hlq_group_norm_act")
+
+
+def hlq_group_norm_act_backward(dY, X, weight, bias, mean, rstd, groups, act, dX, dweight, dbias, workspace=None, p=0.0, seed=0):
+    """dX, dweight, dbias <- gradients of hlq_group_norm_act with the same arguments; any of the three may be None."""
+    Nb, P, C_, pdt = _group_norm_sizes(X, weight, bias, groups)
+    if weight is None and bias is None:
+        pdt = dweight.dtype if dweight is not None else (dbias.dtype if dbias is not None else pdt)
+    _expect_like("dY", dY, X)
+    _expect_like("dX", dX, X)
+    _expect_vector("mean", mean, (Nb, groups), torch.float32)
+    _expect_vector("rstd", rstd, (Nb, groups), torch.float32)
+    _expect_vector("dweight", dweight, (C_,), pdt)
+    _expect_vector("dbias", dbias, (C_,), pdt)
+    wp, wb = _ws(workspace)
+    _check(lib().hlq_group_norm_act_backward(_ptr(dY), _ptr(X), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), Nb, P, C_, groups, act,
+                                             p, seed, _dt(X), _dtype_code(pdt), _ptr(dX), _ptr(dweight), _ptr(dbias), wp, wb, _stream()),
+           "hlq_group_norm_act_backward")
+
+
+def hlq_rel_positions(geom) -> int:
+    """Number of relative positions of a map: the length of `buckets`."""
+    if geom.grid_w:
+        return (2 * (geom.K // geom.grid_w) - 1) * (2 * geom.grid_w - 1)
+    return max(0, geom.Q + geom.K - 1)
+
+
+def _expect_rel(S, table, buckets, mask, geom):
+    if tuple(S.shape) != (geom.B, geom.H, geom.Q, geom.K):
+        raise ValueError("scores must be %s, got %s" % ((geom.B, geom.H, geom.Q, geom.K), tuple(S.shape)))
+    _expect_vector("table", table, (geom.n_buckets, geom.H), table.dtype)
+    _expect_vector("buckets", buckets, (hlq_rel_positions(geom),), torch.int32)
+    if (mask is None) != (geom.mask_batches == 0):
+        raise ValueError("mask and geom.mask_batches do not agree")
+    if mask is not None:
+        if mask.dtype not in (torch.uint8, torch.bool) or tuple(mask.shape) != (geom.mask_batches, geom.mask_rows, geom.K):
+            raise ValueError("mask must be bytes %s, got %s %s" % ((geom.mask_batches, geom.mask_rows, geom.K), mask.dtype, tuple(mask.shape)))
+
+
+def hlq_rel_softmax(S, table, buckets, mask, geom, scale, P, p=0.0, seed=0):
+    """P <- dropout(softmax(scale S + bias)), the bias of a key by its position relative to the query."""
+    _expect_rel(S, table, buckets, mask, geom)
+    _expect_like("P", P, S)
+    _check(lib().hlq_rel_softmax(_ptr(S), _ptr(table), _ptr(buckets), _ptr(mask), C.byref(geom), scale, p, seed, _dt(S), _dt(table),
+                                 _ptr(P), _stream()), "hlq_rel_softmax")
+
+
+def hlq_rel_softmax_workspace_bytes(geom, dtype) -> int:
+    return int(lib().hlq_rel_softmax_workspace_bytes(C.byref(geom), _dtype_code(dtype)))
+
+
+def hlq_rel_softmax_backward(dP, S, table, buckets, mask, geom, scale, dS, dtable=None, workspace=None, p=0.0, seed=0):
+    """dS, dtable <- gradients of hlq_rel_softmax with the same arguments; dtable may be None."""
+    _expect_rel(S, table, buckets, mask, geom)
+    _expect_like("dP", dP, S)
+    _expect_like("dS", dS, S)
+    _expect_vector("dtable", dtable, tuple(table.shape), table.dtype)
+    wp, wb = _ws(workspace)
+    _check(lib().hlq_rel_softmax_backward(_ptr(dP), _ptr(S), _ptr(table), _ptr(buckets), _ptr(mask), C.byref(geom), scale, p, seed, _dt(S),
+                                          _dt(table), _ptr(dS), _ptr(dtable), wp, wb, _stream()), "hlq_rel_softmax_backward")

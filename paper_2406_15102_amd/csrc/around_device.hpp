@@ -1,0 +1,214 @@
+// Device-side building blocks of the operators around the products (group normalisation, dropout, attention map): loads and
+// stores of a few consecutive elements at any element's address, activations and their slopes, which elements dropout
+// keeps, and sums over lanes.
+#pragma once
+#include "hlq_device.hpp"
+#include "hlq_kernels.hpp"
+
+namespace hlq {
+
+// ---- NE consecutive elements as they lie in memory ---------------------------------------------
+// The types are aligned like one element: the hardware takes a 16-byte access at any element's address, so rows of an odd length
+// are read and written in whole vectors as well.
+typedef uint32_t raw4_t __attribute__((ext_vector_type(4)));
+typedef raw4_t raw4_e2 __attribute__((aligned(2)));
+typedef uint32_t raw1_e2 __attribute__((aligned(2)));
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef f4_t f4_e4 __attribute__((aligned(4)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
+typedef f2_t f2_e4 __attribute__((aligned(4)));
+
+template <typename T, int NE> struct Raw;
+template <> struct Raw<bf16_t, 8> {
+    raw4_t w;
+    __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const raw4_e2 *>(p); }
+    __device__ __forceinline__ void zero() { w = raw4_t{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ void widen(float *v) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
+    }
+    static __device__ __forceinline__ void store(bf16_t *p, const float *v)
+    {
+        raw4_t o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<raw4_e2 *>(p) = o;
+    }
+};
+template <> struct Raw<float, 8> {
+    f4_t a, b;
+    __device__ __forceinline__ void load(const float *p)
+    {
+        a = *reinterpret_cast<const f4_e4 *>(p);
+        b = *reinterpret_cast<const f4_e4 *>(p + 4);
+    }
+    __device__ __forceinline__ void zero() { a = b = f4_t{0.0f, 0.0f, 0.0f, 0.0f}; }
+    __device__ __forceinline__ void widen(float *v) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+    static __device__ __forceinline__ void store(float *p, const float *v)
+    {
+        *reinterpret_cast<f4_e4 *>(p) = f4_t{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f4_e4 *>(p + 4) = f4_t{v[4], v[5], v[6], v[7]};
+    }
+};
+template <> struct Raw<bf16_t, 2> {
+    uint32_t w;
+    __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const raw1_e2 *>(p); }
+    __device__ __forceinline__ void zero() { w = 0; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = bf16_lo(w), v[1] = bf16_hi(w); }
+    static __device__ __forceinline__ void store(bf16_t *p, const float *v) { *reinterpret_cast<raw1_e2 *>(p) = pack_bf16(v[0], v[1]); }
+};
+template <> struct Raw<float, 2> {
+    f2_t w;
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const f2_e4 *>(p); }
+    __device__ __forceinline__ void zero() { w = f2_t{0.0f, 0.0f}; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = w[0], v[1] = w[1]; }
+    static __device__ __forceinline__ void store(float *p, const float *v) { *reinterpret_cast<f2_e4 *>(p) = f2_t{v[0], v[1]}; }
+};
+template <> struct Raw<bf16_t, 1> {
+    bf16_t w;
+    __device__ __forceinline__ void load(const bf16_t *p) { w = *p; }
+    __device__ __forceinline__ void zero() { w = 0; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = bf16_lo(w); }
+    static __device__ __forceinline__ void store(bf16_t *p, const float *v) { *p = static_cast<bf16_t>(pack_bf16(v[0], 0.0f) & 0xFFFFu); }
+};
+template <> struct Raw<float, 1> {
+    float w;
+    __device__ __forceinline__ void load(const float *p) { w = *p; }
+    __device__ __forceinline__ void zero() { w = 0.0f; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = w; }
+    static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
+};
+
+template <typename T> __device__ __forceinline__ float load_one(const T *p)
+{
+    float v;
+    Raw<T, 1> r;
+    r.load(p);
+    r.widen(&v);
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_one(T *p, float v) { Raw<T, 1>::store(p, &v); }
+
+// a layer's parameter, which has an element type of its own
+__device__ __forceinline__ float load_param(const void *p, bool f32, int64_t i)
+{
+    return f32 ? static_cast<const float *>(p)[i] : load_one(static_cast<const bf16_t *>(p) + i);
+}
+__device__ __forceinline__ void store_param(void *p, bool f32, int64_t i, float v)
+{
+    if (f32) static_cast<float *>(p)[i] = v;
+    else store_one(static_cast<bf16_t *>(p) + i, v);
+}
+
+// ---- exponential and sigmoid -------------------------------------------------------------------
+// EXACT (fp32 tensors): within 2 units in the last place.  Else (results that are rounded to bf16) the hardware's base-2
+// exponential and reciprocal, one unit each, on an argument rounded once: 1e-5 relative at |x| = 88.
+template <bool EXACT> __device__ __forceinline__ float exp_of(float x)
+{
+    return EXACT ? expf(x) : __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
+}
+template <bool EXACT> __device__ __forceinline__ float recip_of(float x) { return EXACT ? 1.0f / x : __builtin_amdgcn_rcpf(x); }
+
+// ---- activations (HLQ_ACT_*) -------------------------------------------------------------------
+template <bool EXACT, int NE>
+__device__ __forceinline__ void act_values(float *z, int act)
+{
+    if (act == 1) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) z[e] = z[e] < 0.0f ? 0.0f : z[e];       // keeps a NaN
+    } else if (act == 2) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) z[e] *= recip_of<EXACT>(1.0f + exp_of<EXACT>(-z[e]));
+    } else if (act == 3) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) z[e] = 0.5f * z[e] * (1.0f + erff(z[e] * 0.70710678118654752f));
+    }
+}
+// d[e] *= slope of the activation at z[e]
+template <bool EXACT, int NE>
+__device__ __forceinline__ void act_slopes(const float *z, int act, float *d)
+{
+    if (act == 1) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) d[e] = z[e] > 0.0f ? d[e] : 0.0f;
+    } else if (act == 2) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            const float s = recip_of<EXACT>(1.0f + exp_of<EXACT>(-z[e]));
+            d[e] *= s * __builtin_fmaf(z[e], 1.0f - s, 1.0f);
+        }
+    } else if (act == 3) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            const float cdf = 0.5f * (1.0f + erff(z[e] * 0.70710678118654752f));
+            d[e] *= __builtin_fmaf(z[e] * 0.39894228040143268f, exp_of<EXACT>(-0.5f * z[e] * z[e]), cdf);
+        }
+    }
+}
+
+// ---- dropout -----------------------------------------------------------------------------------
+// Element i is dropped where half i & 1 (the low one first) of word i >> 1 of the stream is below `below` (= 65536 p rounded to
+// a whole number), else multiplied by `scale` = 65536 / (65536 - below).  below = 0: there is no dropout.
+// v[0 .. NE) are elements i .. i + NE - 1, i a multiple of NE (NE = 1, 2 or 8).  A dropped element is 0 whatever it was.
+template <int NE>
+__device__ __forceinline__ void drop_values(float *v, int64_t i, const DropRule &d)
+{
+    if constexpr (NE == 1) {
+        uint32_t w;
+        rand_words<1>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, &w);
+        const uint32_t u = (i & 1) ? w >> 16 : w & 0xFFFFu;
+        v[0] = u >= d.below ? v[0] * d.scale : 0.0f;
+    } else {
+        constexpr int NW = NE / 2;
+        uint32_t w[NW];
+        rand_words<NW>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, w);
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            v[2 * k] = (w[k] & 0xFFFFu) >= d.below ? v[2 * k] * d.scale : 0.0f;
+            v[2 * k + 1] = (w[k] >> 16) >= d.below ? v[2 * k + 1] * d.scale : 0.0f;
+        }
+    }
+}
+
+// ---- sums and maxima over aligned groups of LANES lanes of a wavefront ---------------------------
+// Steps of 1 and 2 are quad permutes, 4 and 8 mirrors of half rows and rows (after the smaller steps all lanes of a quad,
+// of a half row, hold the same), 16 a swizzle, 32 a permute.
+template <int STEP> __device__ __forceinline__ float lane_partner(float x)
+{
+    const int i = __builtin_bit_cast(int, x);
+    int r;
+    if constexpr (STEP == 1) r = __builtin_amdgcn_update_dpp(0, i, 0xB1, 0xF, 0xF, true);          // quad_perm [1,0,3,2]
+    else if constexpr (STEP == 2) r = __builtin_amdgcn_update_dpp(0, i, 0x4E, 0xF, 0xF, true);     // quad_perm [2,3,0,1]
+    else if constexpr (STEP == 4) r = __builtin_amdgcn_update_dpp(0, i, 0x141, 0xF, 0xF, true);    // row_half_mirror
+    else if constexpr (STEP == 8) r = __builtin_amdgcn_update_dpp(0, i, 0x140, 0xF, 0xF, true);    // row_mirror
+    else if constexpr (STEP == 16) r = __builtin_amdgcn_ds_swizzle(i, 0x401F);                     // lane ^ 16
+    else r = __shfl_xor(i, 32);
+    return __builtin_bit_cast(float, r);
+}
+template <int LANES> __device__ __forceinline__ float lanes_sum(float x)
+{
+    if constexpr (LANES >= 2) x += lane_partner<1>(x);
+    if constexpr (LANES >= 4) x += lane_partner<2>(x);
+    if constexpr (LANES >= 8) x += lane_partner<4>(x);
+    if constexpr (LANES >= 16) x += lane_partner<8>(x);
+    if constexpr (LANES >= 32) x += lane_partner<16>(x);
+    if constexpr (LANES >= 64) x += lane_partner<32>(x);
+    return x;
+}
+template <int LANES> __device__ __forceinline__ float lanes_max(float x)
+{
+    if constexpr (LANES >= 2) x = fmaxf(x, lane_partner<1>(x));
+    if constexpr (LANES >= 4) x = fmaxf(x, lane_partner<2>(x));
+    if constexpr (LANES >= 8) x = fmaxf(x, lane_partner<4>(x));
+    if constexpr (LANES >= 16) x = fmaxf(x, lane_partner<8>(x));
+    if constexpr (LANES >= 32) x = fmaxf(x, lane_partner<16>(x));
+    if constexpr (LANES >= 64) x = fmaxf(x, lane_partner<32>(x));
+    return x;
+}
+
+}  // namespace hlq

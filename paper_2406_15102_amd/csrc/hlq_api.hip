@@ -1131,4 +1131,181 @@ int hlq_conv2d_backward(const void *G, const void *X, const void *Wt, const hlq_
     return HLQ_OK;
 }
 
+// ---- operators around the products ------------------------------------------------------------
+
+namespace {
+
+constexpr uint32_t kDropTensor = 4;      // the stream that drops: one key for every operator, so a fused pass drops what the separate one does
+
+// p and seed as the kernels take them; `n` elements of the stream are used
+int drop_rule(double p, uint64_t seed, int64_t n, hlq::DropRule *d)
+{
+    if (!(p >= 0.0 && p <= 1.0)) return HLQ_ERR_SHAPE;
+    d->below = static_cast<uint32_t>(65536.0 * p + 0.5);
+    d->scale = d->below < 65536u ? static_cast<float>(65536.0 / (65536.0 - d->below)) : 0.0f;
+    const uint64_t key = stream_key(seed, kDropTensor);
+    d->k0 = static_cast<uint32_t>(key), d->k1 = static_cast<uint32_t>(key >> 32);
+    if (d->below && n > (int64_t(1) << 33)) return HLQ_ERR_SHAPE;      // a word of the 32-bit counter to two elements
+    return HLQ_OK;
+}
+
+size_t element_bytes(int dtype) { return dtype == HLQ_F32 ? 4 : 2; }
+
+int check_group_norm(int64_t Nb, int64_t P, int64_t C, int64_t groups)
+{
+    if (Nb < 0 || P <= 0 || C <= 0 || groups <= 0 || C % groups != 0) return HLQ_ERR_SHAPE;
+    if (C > (int64_t(1) << 24) || P > (int64_t(1) << 40) / C || Nb >= (int64_t(1) << 31) / C) return HLQ_ERR_SHAPE;
+    if (Nb > 0 && P * C > (int64_t(1) << 48) / Nb) return HLQ_ERR_SHAPE;
+    if (!hlq::group_norm_ok(static_cast<int>(C), static_cast<int>(C / groups))) return HLQ_ERR_SHAPE;
+    return HLQ_OK;
+}
+
+int group_norm_args(const void *X, const void *weight, const void *bias, int64_t Nb, int64_t P, int64_t C, int64_t groups, int act, double p,
+                    uint64_t seed, int dtype, int param_dtype, hlq::GroupNormArgs *a)
+{
+    int rc;
+    if ((rc = check_dtype(dtype)) != HLQ_OK || (rc = check_dtype(param_dtype)) != HLQ_OK) return rc;
+    if ((rc = check_group_norm(Nb, P, C, groups)) != HLQ_OK) return rc;
+    if (act < HLQ_ACT_NONE || act > HLQ_ACT_GELU) return HLQ_ERR_SHAPE;
+    if ((rc = drop_rule(p, seed, Nb * P * C, &a->drop)) != HLQ_OK) return rc;
+    const size_t e = element_bytes(dtype), pe = element_bytes(param_dtype);
+    if (!aligned(X, e) || !aligned(weight, pe) || !aligned(bias, pe)) return HLQ_ERR_SHAPE;
+    a->x = X, a->w = weight, a->b = bias;
+    a->P = P, a->Nb = static_cast<int>(Nb), a->C = static_cast<int>(C), a->groups = static_cast<int>(groups), a->cg = static_cast<int>(C / groups);
+    a->act = act, a->is_f32 = dtype == HLQ_F32, a->param_f32 = param_dtype == HLQ_F32;
+    return HLQ_OK;
+}
+
+// scratch of a call that needs `need` bytes: the caller's, or the registered or library-owned one
+int scratch(size_t need, void *workspace, size_t workspace_bytes, void **out)
+{
+    *out = workspace;
+    if (need == 0) return HLQ_OK;
+    if (workspace) return workspace_bytes >= need && aligned(workspace, 256) ? HLQ_OK : HLQ_ERR_WORKSPACE;
+    size_t have = 0;
+    return own_workspace(need, need, out, &have);
+}
+
+int rel_args(const void *S, const void *table, const int32_t *buckets, const uint8_t *mask, const hlq_rel_geom *g, float scale, double p,
+             uint64_t seed, int dtype, int table_dtype, hlq::RelArgs *a)
+{
+    int rc;
+    if (!g) return HLQ_ERR_NULL;
+    if ((rc = check_dtype(dtype)) != HLQ_OK || (rc = check_dtype(table_dtype)) != HLQ_OK) return rc;
+    if (g->B < 0 || g->Q < 0 || g->K < 0 || g->H <= 0 || g->H > 65535 || g->n_buckets <= 0 || g->grid_w < 0) return HLQ_ERR_SHAPE;
+    if (g->Q > (1 << 30) || !hlq::rel_softmax_ok(g->K, g->grid_w)) return HLQ_ERR_SHAPE;
+    if (g->n_buckets > (1 << 24) || (g->causal != 0 && g->causal != 1)) return HLQ_ERR_SHAPE;
+    if (g->grid_w && (g->Q != g->K || g->K % g->grid_w != 0)) return HLQ_ERR_SHAPE;
+    if (g->mask_batches < 0 || (g->mask_batches == 0 && g->mask_rows != 0)) return HLQ_ERR_SHAPE;
+    if (g->mask_batches && g->mask_rows != 1 && g->mask_rows != g->Q) return HLQ_ERR_SHAPE;
+    const int64_t rows = static_cast<int64_t>(g->B) * g->H;          // < 2^47
+    if (g->Q > 0 && rows > (int64_t(1) << 46) / g->Q) return HLQ_ERR_SHAPE;
+    if ((rc = drop_rule(p, seed, rows * g->Q * ((g->K + 7) / 8 * 8), &a->drop)) != HLQ_OK) return rc;
+    const bool empty = g->B == 0 || g->Q == 0 || g->K == 0;
+    if (!empty && (!S || !table || !buckets || (g->mask_batches && !mask))) return HLQ_ERR_NULL;
+    if (!aligned(S, element_bytes(dtype)) || !aligned(table, element_bytes(table_dtype)) || !aligned(buckets, 4)) return HLQ_ERR_SHAPE;
+    a->s = S, a->table = table, a->of = buckets, a->mask = g->mask_batches ? mask : nullptr;
+    a->B = g->B, a->H = g->H, a->Q = g->Q, a->K = g->K, a->grid_w = g->grid_w, a->n_buckets = g->n_buckets, a->causal = g->causal;
+    a->mask_batches = g->mask_batches, a->mask_rows = g->mask_rows;
+    a->is_f32 = dtype == HLQ_F32, a->param_f32 = table_dtype == HLQ_F32, a->scale = scale;
+    return HLQ_OK;
+}
+
+}  // namespace
+
+int hlq_dropout(const void *X, const void *residual, int64_t n, double p, uint64_t seed, int dtype, void *Y, void *stream)
+{
+    int rc;
+    hlq::DropRule d;
+    if ((rc = check_dtype(dtype)) != HLQ_OK) return rc;
+    if (n < 0 || n > (int64_t(1) << 40)) return HLQ_ERR_SHAPE;
+    if ((rc = drop_rule(p, seed, n, &d)) != HLQ_OK) return rc;
+    if (n == 0) return HLQ_OK;
+    if (!X || !Y) return HLQ_ERR_NULL;
+    const size_t e = element_bytes(dtype);
+    if (!aligned(X, e) || !aligned(Y, e) || !aligned(residual, e)) return HLQ_ERR_SHAPE;
+    return launch_rc(hlq::launch_dropout(X, residual, n, dtype == HLQ_F32, d, Y, static_cast<hipStream_t>(stream)));
+}
+
+size_t hlq_group_norm_workspace_bytes(int64_t Nb, int64_t P, int64_t C, int64_t groups, int dtype, int backward)
+{
+    if (check_dtype(dtype) != HLQ_OK || check_group_norm(Nb, P, C, groups) != HLQ_OK) return 0;
+    return hlq::group_norm_ws_bytes(Nb, P, static_cast<int>(C), static_cast<int>(groups), dtype == HLQ_F32, backward != 0);
+}
+
+int hlq_group_norm_act(const void *X, const void *weight, const void *bias, int64_t Nb, int64_t P, int64_t C, int64_t groups, float eps, int act,
+                       double p, uint64_t seed, int dtype, int param_dtype, void *Y, float *mean, float *rstd, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    int rc;
+    hlq::GroupNormArgs a{};
+    if ((rc = group_norm_args(X, weight, bias, Nb, P, C, groups, act, p, seed, dtype, param_dtype, &a)) != HLQ_OK) return rc;
+    if (!(eps > 0.0f)) return HLQ_ERR_SHAPE;
+    if (Nb == 0) return HLQ_OK;
+    if (!X || !Y) return HLQ_ERR_NULL;
+    if (!aligned(Y, element_bytes(dtype)) || !aligned(mean, 4) || !aligned(rstd, 4)) return HLQ_ERR_SHAPE;
+    a.y = Y, a.mean = mean, a.rstd = rstd, a.eps = eps;
+    const size_t need = hlq::group_norm_ws_bytes(Nb, P, a.C, a.groups, a.is_f32, false);
+    if ((rc = scratch(need, workspace, workspace_bytes, &a.ws)) != HLQ_OK) return rc;
+    return launch_rc(hlq::launch_group_norm(a, static_cast<hipStream_t>(stream)));
+}
+
+int hlq_group_norm_act_backward(const void *dY, const void *X, const void *weight, const void *bias, const float *mean, const float *rstd,
+                                int64_t Nb, int64_t P, int64_t C, int64_t groups, int act, double p, uint64_t seed, int dtype, int param_dtype,
+                                void *dX, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc;
+    hlq::GroupNormArgs a{};
+    if ((rc = group_norm_args(X, weight, bias, Nb, P, C, groups, act, p, seed, dtype, param_dtype, &a)) != HLQ_OK) return rc;
+    if (Nb > 0 && (!dY || !X || !mean || !rstd)) return HLQ_ERR_NULL;
+    if (!dX && !dweight && !dbias) return HLQ_ERR_NULL;
+    const size_t e = element_bytes(dtype), pe = element_bytes(param_dtype);
+    if (!aligned(dY, e) || !aligned(dX, e) || !aligned(dweight, pe) || !aligned(dbias, pe) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return HLQ_ERR_SHAPE;
+    if (Nb == 0 && !dweight && !dbias) return HLQ_OK;
+    a.dy = dY, a.y = dX, a.dw = dweight, a.db = dbias, a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
+    const size_t need = hlq::group_norm_ws_bytes(Nb, P, a.C, a.groups, a.is_f32, true);
+    if ((rc = scratch(need, workspace, workspace_bytes, &a.ws)) != HLQ_OK) return rc;
+    return launch_rc(hlq::launch_group_norm_backward(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t hlq_rel_softmax_workspace_bytes(const hlq_rel_geom *g, int dtype)
+{
+    hlq::RelArgs a{};
+    static const int32_t some[4] = {0, 0, 0, 0};       // stands for the tensors, which are not read
+    if (rel_args(some, some, some, reinterpret_cast<const uint8_t *>(some), g, 1.0f, 0.0, 0, dtype, HLQ_F32, &a) != HLQ_OK) return 0;
+    return hlq::rel_softmax_ws_bytes(a);
+}
+
+int hlq_rel_softmax(const void *S, const void *table, const int32_t *buckets, const uint8_t *mask, const hlq_rel_geom *g, float scale, double p,
+                    uint64_t seed, int dtype, int table_dtype, void *Pm, void *stream)
+{
+    int rc;
+    hlq::RelArgs a{};
+    if ((rc = rel_args(S, table, buckets, mask, g, scale, p, seed, dtype, table_dtype, &a)) != HLQ_OK) return rc;
+    if (a.B == 0 || a.Q == 0 || a.K == 0) return HLQ_OK;
+    if (!Pm) return HLQ_ERR_NULL;
+    if (!aligned(Pm, element_bytes(dtype))) return HLQ_ERR_SHAPE;
+    a.out = Pm;
+    return launch_rc(hlq::launch_rel_softmax(a, static_cast<hipStream_t>(stream)));
+}
+
+int hlq_rel_softmax_backward(const void *dP, const void *S, const void *table, const int32_t *buckets, const uint8_t *mask, const hlq_rel_geom *g,
+                             float scale, double p, uint64_t seed, int dtype, int table_dtype, void *dS, void *dtable, void *workspace,
+                             size_t workspace_bytes, void *stream)
+{
+    int rc;
+    hlq::RelArgs a{};
+    if ((rc = rel_args(S, table, buckets, mask, g, scale, p, seed, dtype, table_dtype, &a)) != HLQ_OK) return rc;
+    const bool empty = a.B == 0 || a.Q == 0 || a.K == 0;
+    if (!empty && (!dP || !dS)) return HLQ_ERR_NULL;
+    if (!aligned(dP, element_bytes(dtype)) || !aligned(dS, element_bytes(dtype)) || !aligned(dtable, element_bytes(table_dtype))) return HLQ_ERR_SHAPE;
+    if (empty && !dtable) return HLQ_OK;
+    a.dp = dP, a.out = dS, a.dtable = dtable;
+    void *ws = nullptr;
+    if ((rc = scratch(hlq::rel_softmax_ws_bytes(a), workspace, workspace_bytes, &ws)) != HLQ_OK) return rc;
+    a.ws = static_cast<float *>(ws);
+    return launch_rc(hlq::launch_rel_softmax_backward(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

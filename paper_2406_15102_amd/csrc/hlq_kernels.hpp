@@ -376,6 +376,53 @@ hipError_t launch_hla_conv(const void *X, const ConvShape &g, int B, int r, int 
 hipError_t launch_hla_quant_conv(const void *X, const ConvShape &g, int B, int r, int basis, bool is_f32, uint32_t k0,
                                  uint32_t k1, bool mant, int8_t *TqT, float *sT, float *coeffT, void *ws, hipStream_t st);
 
+// ---- operators around the products ------------------------------------------------------------
+// Dropout by the counter stream (around_device.hpp): below = 65536 p as a whole number, scale = 65536 / (65536 - below).
+struct DropRule {
+    uint32_t k0, k1, below;
+    float scale;
+};
+// y = r + dropout(x) over n elements; r NULL: no residual.  y may be x or r.
+hipError_t launch_dropout(const void *x, const void *r, int64_t n, bool is_f32, const DropRule &d, void *y, hipStream_t st);
+
+// Group normalisation, activation and dropout of channels-last x [Nb, P, C] (k_group_norm.hip).
+struct GroupNormArgs {
+    const void *x, *dy, *w, *b;      // dy: backward only; w, b [C] or NULL (ones, zeros)
+    float *mean, *rstd;              // [Nb, groups]: forward writes them (NULL: not wanted), backward reads them
+    void *y;                         // forward: y; backward: dx (NULL: not wanted)
+    void *dw, *db;                   // backward: [C] or NULL
+    void *ws;
+    int64_t P;
+    int Nb, C, groups, cg, act;      // cg: channels of a group
+    bool is_f32, param_f32;
+    float eps;
+    DropRule drop;
+};
+// false: no kernel takes channels grouped so
+bool group_norm_ok(int C, int cg);
+size_t group_norm_ws_bytes(int64_t Nb, int64_t P, int C, int groups, bool is_f32, bool backward);
+hipError_t launch_group_norm(const GroupNormArgs &a, hipStream_t st);
+hipError_t launch_group_norm_backward(const GroupNormArgs &a, hipStream_t st);
+
+// Attention map with a relative position bias (k_rel_softmax.hip): s, dp, out [B, H, Q, K].
+struct RelArgs {
+    const void *s, *dp;              // dp: backward only
+    const void *table;               // [n_buckets, H]
+    const int32_t *of;               // bucket of every relative position
+    const uint8_t *mask;             // [mask_batches, mask_rows, K] or NULL
+    void *out;                       // forward: the map; backward: gradient of s
+    void *dtable;                    // backward: [n_buckets, H] or NULL
+    float *ws;
+    int B, H, Q, K, grid_w, n_buckets, causal, mask_batches, mask_rows;
+    bool is_f32, param_f32;
+    float scale;
+    DropRule drop;
+};
+bool rel_softmax_ok(int K, int grid_w);      // a row that long is taken
+size_t rel_softmax_ws_bytes(const RelArgs &a);
+hipError_t launch_rel_softmax(const RelArgs &a, hipStream_t st);
+hipError_t launch_rel_softmax_backward(const RelArgs &a, hipStream_t st);
+
 // Diagnostic: `blocks` workgroups of 4 wavefronts each run `iters` x 8 independent 32x32 MFMAs
 // (kind 0: i8, K = 32; kind 1: bf16, K = 16) from registers.
 hipError_t launch_mfma_probe(int kind, int blocks, int iters, float *sink, hipStream_t st);

@@ -1,0 +1,214 @@
+"""hlq_group_norm_act and its gradients against the 64-bit definition: groups of one channel to all of them, channels that no
+vector divides, maps of one position to ones in many chunks, both types of tensors and parameters, maps far off zero."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_15102_amd as hlq
+from oracle import around_oracle as ao
+from paper_2406_15102_amd.autograd import HlqGroupNormAct, HlqGroupNormActFunction
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24
+
+
+def _half(dtype):
+    return 2.0 ** -8 if dtype == BF16 else U
+
+
+def _inputs(Nb, P, C, dtype, pdt, seed, shift=0.5):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn((Nb, P, C), generator=g) * (0.5 + torch.rand(C, generator=g)) + shift * torch.randn(C, generator=g)).to(dtype)
+    w, b = (1 + 0.3 * torch.randn(C, generator=g)).to(pdt), (0.3 * torch.randn(C, generator=g)).to(pdt)
+    dy = torch.randn((Nb, P, C), generator=g).to(dtype)
+    return x, w, b, dy
+
+
+def _run(x, w, b, dy, groups, act, p, seed, eps=1e-5):
+    Nb, P, C = x.shape
+    X, DY = x.to(DEV), dy.to(DEV)
+    W, B = (None if t is None else t.to(DEV) for t in (w, b))
+    Y, DX = torch.empty_like(X), torch.empty_like(X)
+    mean, rstd = (torch.empty((Nb, groups), device=DEV) for _ in range(2))
+
+    def ws(back):
+        n = hlq.hlq_group_norm_workspace_bytes(Nb, P, C, groups, x.dtype, back)
+        return torch.empty(n, dtype=torch.uint8, device=DEV) if n else None
+
+    hlq.hlq_group_norm_act(X, W, B, groups, eps, act, Y, mean, rstd, ws(False), p, seed)
+    pdt = F32 if w is None else w.dtype
+    dw, db = (torch.empty(C, dtype=pdt, device=DEV) for _ in range(2))
+    hlq.hlq_group_norm_act_backward(DY, X, W, B, mean, rstd, groups, act, DX, dw, db, ws(True), p, seed)
+    return Y, mean, rstd, DX, dw, db
+
+
+def _compare(x, w, b, dy, groups, act, p, seed, out, eps=1e-5):
+    """fp32 arithmetic: every sum has at most 256 additions in a row (64 of a thread, 8 and 128 of the columns, 256 chunks and as many
+    rows of partial sums at most, none of them with all of the others), each of half a unit of the sum of magnitudes; statistics take the
+    error of the mean to the difference from it, an error of |x| rstd units.  Held to 64 units of those magnitudes, where the errors
+    of a sum were all of one sign."""
+    x64, dy64 = x.double().numpy(), dy.double().numpy()
+    w64 = None if w is None else w.double().numpy()
+    b64 = None if b is None else b.double().numpy()
+    Y, mean, rstd, DX, dw, db = (t.double().cpu().numpy() for t in out)
+    y, m, r = ao.group_norm_act(x64, w64, b64, groups, eps, act, p, seed)
+    dx, gw, gb = ao.group_norm_act_backward(dy64, x64, w64, b64, groups, eps, act, p, seed)
+    Nb, P, C = x.shape
+    cg = C // groups
+    top = np.abs(x64).reshape(Nb, P, groups, cg).max((1, 3))
+    assert np.all(np.abs(mean - m) <= 64 * U * top)
+    assert np.all(np.abs(rstd - r) <= 64 * U * r * (1 + top * r))
+    wide = np.repeat(top * r, cg, 1)[:, None, :]                       # |x| rstd
+    wa = np.ones(C) if w64 is None else np.abs(w64)
+    ba = np.zeros(C) if b64 is None else np.abs(b64)
+    keep = 65536 / (65536 - int(65536 * p + 0.5)) if p < 1 else 1.0
+    fast = 2.0 ** -16 if x.dtype == BF16 else 0.0                      # the hardware's exponential on a rounded argument
+    err = (64 * U * (1 + wide) + fast) * (wa * (1 + wide) + ba) * keep
+    half = _half(x.dtype)
+    bad = np.abs(Y - y) - (half * np.abs(y) + err * 2)
+    assert np.all(bad <= 0), float(bad.max())
+    big = np.abs(dy64).max() * keep * 1.2                              # |dz|: slopes are at most 1.13
+    e = 64 * U * (1 + wide) ** 2 + fast
+    # an input of the activation that the forward error moves moves the slope by at most one unit of z; relu's slope jumps: leave its edge out
+    z = (x64 - np.repeat(m, cg, 1)[:, None]) * np.repeat(r, cg, 1)[:, None] * (1 if w64 is None else w64) + (0 if b64 is None else b64)
+    edge = (np.abs(z) <= err) if act == 1 else np.zeros(z.shape, bool)
+    jump = edge.reshape(Nb, P, groups, cg).sum((1, 3)) / (P * cg)
+    slack = np.repeat(np.repeat(r, cg, 1)[:, None] * big * wa * (1 + wide), 1, 1) * (np.repeat(jump, cg, 1)[:, None] * (1 + wide))
+    bound = half * np.abs(dx) + np.repeat(r, cg, 1)[:, None] * big * (wa + np.abs(wa).max()) * e * 4 + slack
+    bad = np.where(edge, 0, np.abs(DX - dx) - bound)
+    assert np.all(bad <= 0), float(bad.max())
+    ph = U if w is None else _half(w.dtype)
+    n = Nb * P
+    edges = edge.sum((0, 1)) * big
+    assert np.all(np.abs(db - gb) <= ph * np.abs(gb) + e.max() * big * np.sqrt(n) * 4 + edges)
+    assert np.all(np.abs(dw - gw) <= ph * np.abs(gw) + e.max() * big * np.sqrt(n) * 16 + edges * (1 + wide.max()))
+
+
+# C, groups: a vector of 8, of 2, of 1; groups of one channel, of six in vectors, of more channels than 128 bytes; several slabs, a ragged one
+CHANNELS = [(8, 1), (8, 8), (64, 16), (64, 2), (96, 16), (80, 8), (320, 32), (90, 15), (30, 10), (33, 11), (7, 1), (1, 1), (200, 25), (520, 1),
+            (1024, 2), (2048, 1)]
+
+
+@pytest.mark.parametrize("C,groups", CHANNELS)
+@pytest.mark.parametrize("P", [1, 3, 49, 300])
+@pytest.mark.parametrize("dtype,pdt", [(BF16, F32), (F32, BF16)])
+def test_channels_and_groups(C, groups, P, dtype, pdt):
+    if P * (C // groups) < 2:
+        pytest.skip("a group of one value has no variance: everything is bias")
+    act = (C + P) % 4
+    x, w, b, dy = _inputs(3, P, C, dtype, pdt, C + P)
+    _compare(x, w, b, dy, groups, act, 0.0, 1, _run(x, w, b, dy, groups, act, 0.0, 1))
+
+
+@pytest.mark.parametrize("act", [0, 1, 2, 3])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C,groups,P", [(64, 8, 196), (90, 15, 70), (5, 5, 40)])
+def test_activations_with_dropout(act, dtype, C, groups, P):
+    x, w, b, dy = _inputs(2, P, C, dtype, dtype, act)
+    _compare(x, w, b, dy, groups, act, 0.25, 3, _run(x, w, b, dy, groups, act, 0.25, 3))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Nb,P,C,groups", [(1, 5000, 64, 32), (2, 4099, 80, 8), (1, 20001, 6, 3), (3, 2500, 65, 5), (1, 70000, 16, 1), (2, 1100, 1024, 8)])
+def test_maps_in_chunks(Nb, P, C, groups, dtype):
+    x, w, b, dy = _inputs(Nb, P, C, dtype, F32, P)
+    _compare(x, w, b, dy, groups, 2, 0.1, 3, _run(x, w, b, dy, groups, 2, 0.1, 3))
+
+
+@pytest.mark.parametrize("P", [60, 6000])
+@pytest.mark.parametrize("first", [0.0, 1000.0, 1e6])
+def test_far_off_zero(P, first):
+    """Mean 1000 spread 1 in fp32, the first position apart from the rest: no difference of large sums."""
+    x, w, b, dy = _inputs(2, P, 32, F32, F32, 9, shift=0.0)
+    x += 1000.0
+    x[:, 0] = first
+    _compare(x, w, b, dy, 4, 0, 0.0, 0, _run(x, w, b, dy, 4, 0, 0.0, 0))
+
+
+def test_without_parameters_and_constant_maps():
+    x, _, _, dy = _inputs(2, 50, 24, F32, F32, 4)
+    _compare(x, None, None, dy, 3, 2, 0.0, 0, _run(x, None, None, dy, 3, 2, 0.0, 0))
+    x = torch.full((2, 50, 24), 3.25)
+    out = _run(x, None, None, dy, 3, 0, 0.0, 0)
+    assert bool((out[0] == 0).all()) and bool((out[1] == 3.25).all()) and bool(torch.isfinite(out[3]).all())
+
+
+def test_parts_of_the_gradient_and_no_images():
+    x, w, b, dy = _inputs(2, 3000, 64, BF16, F32, 4)
+    for P in (100, 3000):
+        X, DY, W, B = x[:, :P].contiguous().to(DEV), dy[:, :P].contiguous().to(DEV), w.to(DEV), b.to(DEV)
+        Y, mean, rstd, DX, dw, db = _run(x[:, :P].contiguous(), w, b, dy[:, :P].contiguous(), 8, 2, 0.1, 3)
+        dx2, dw2, db2 = torch.empty_like(DX), torch.empty_like(dw), torch.empty_like(db)
+        hlq.hlq_group_norm_act_backward(DY, X, W, B, mean, rstd, 8, 2, dx2, None, None, None, 0.1, 3)
+        hlq.hlq_group_norm_act_backward(DY, X, W, B, mean, rstd, 8, 2, None, dw2, None, None, 0.1, 3)
+        hlq.hlq_group_norm_act_backward(DY, X, W, B, mean, rstd, 8, 2, None, None, db2, None, 0.1, 3)
+        assert torch.equal(dx2, DX) and torch.equal(dw2, dw) and torch.equal(db2, db)
+        y2 = torch.empty_like(Y)
+        hlq.hlq_group_norm_act(X, W, B, 8, 1e-5, 2, y2, None, None, None, 0.1, 3)
+        assert torch.equal(y2, Y)
+        none = torch.empty((0, P, 64), dtype=BF16, device=DEV)
+        st = torch.empty((0, 8), device=DEV)
+        hlq.hlq_group_norm_act(none, W, B, 8, 1e-5, 2, none.clone(), st, st)
+        hlq.hlq_group_norm_act_backward(none, none, W, B, st, st, 8, 2, none.clone(), dw2, db2)
+        assert not bool(dw2.any()) and not bool(db2.any())
+
+
+def test_any_address_repeats_and_drops_like_dropout():
+    Nb, P, C = 2, 77, 40
+    x, w, b, dy = _inputs(Nb, P, C, BF16, F32, 2)
+    ref = _run(x, w, b, dy, 5, 2, 0.2, 6)
+    again = _run(x, w, b, dy, 5, 2, 0.2, 6)
+    assert all(torch.equal(a, c) for a, c in zip(ref, again))
+    n = Nb * P * C
+    big = torch.zeros(n + 16, dtype=BF16, device=DEV)
+    for off in (1, 3, 6):
+        X, Y = big[off:off + n].view(Nb, P, C), torch.zeros(n + 16, dtype=BF16, device=DEV)[off + 1:off + 1 + n].view(Nb, P, C)
+        X.copy_(x)
+        hlq.hlq_group_norm_act(X, w.to(DEV), b.to(DEV), 5, 1e-5, 2, Y, None, None, None, 0.2, 6)
+        assert torch.equal(Y, ref[0])
+    plain = _run(x.float(), w, b, dy.float(), 5, 2, 0.0, 6)[0]
+    dropped = torch.empty_like(plain)
+    hlq.hlq_dropout(plain, None, 0.2, 6, dropped)
+    fused = _run(x.float(), w, b, dy.float(), 5, 2, 0.2, 6)[0]
+    assert torch.equal(dropped, fused)
+
+
+def test_places_beyond_32_bits():
+    Nb, P, C, groups = 3, 180000, 4096, 64             # 2.2e9 elements
+    x = torch.empty((Nb, P, C), dtype=BF16, device=DEV)
+    for n in range(Nb):
+        x[n].normal_()
+    y = torch.empty_like(x)
+    w, b = torch.ones(C, device=DEV), torch.zeros(C, device=DEV)
+    hlq.hlq_group_norm_act(x, w, b, groups, 1e-5, 0, y, None, None)
+    last = torch.empty_like(x[:1])
+    hlq.hlq_group_norm_act(x[2:], w, b, groups, 1e-5, 0, last, None, None)
+    # the same image in other chunks: statistics agree to 64 units, the rounding to bf16 may go the other way
+    d = (y[2, -2000:].float() - last[0, -2000:].float()).abs()
+    assert float((d / last[0, -2000:].float().abs().clamp(min=1e-3)).max()) <= 2.0 ** -7
+    v = x[2, :, :64].double()
+    want = (v - v.mean()) / v.var(unbiased=False).add(1e-5).sqrt()
+    assert float((y[2, :, :64].double() - want).abs().max()) <= 2.0 ** -8 * float(want.abs().max()) * 1.01
+
+
+def test_wrapper_and_module():
+    m = HlqGroupNormAct(8, 64, act="silu", p=0.1, device=DEV)
+    x = torch.randn((2, 64, 9, 11), device=DEV).to(BF16).contiguous(memory_format=torch.channels_last).requires_grad_()
+    y = m(x)
+    assert y.shape == x.shape and y.is_contiguous(memory_format=torch.channels_last)
+    gy = torch.randn_like(y)
+    y.backward(gy)
+    xl, gl = (t.detach().permute(0, 2, 3, 1).reshape(2, 99, 64).cpu() for t in (x, gy))
+    out = _run(xl.contiguous(), m.weight.detach().cpu(), m.bias.detach().cpu(), gl.contiguous(), 8, 2, 0.1, m.seed + 1)
+    for got, want in ((y.detach().permute(0, 2, 3, 1), out[0]), (x.grad.permute(0, 2, 3, 1), out[3])):
+        assert torch.equal(got.reshape(2, 99, 64), want)
+    assert torch.equal(m.weight.grad, out[4]) and torch.equal(m.bias.grad, out[5])
+    m.eval()
+    a, c = m(x), m(x)
+    assert torch.equal(a, c)
+    with pytest.raises(ValueError):
+        HlqGroupNormAct(7, 64, device=DEV)
+    z = HlqGroupNormActFunction.apply(x, None, None, 4)
+    assert torch.isfinite(z.float()).all()
