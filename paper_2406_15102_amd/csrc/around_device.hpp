@@ -12,6 +12,7 @@ namespace hlq {
 // are read and written in whole vectors as well.
 typedef uint32_t raw4_t __attribute__((ext_vector_type(4)));
 typedef raw4_t raw4_e2 __attribute__((aligned(2)));
+typedef uint32_t raw2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t raw1_e2 __attribute__((aligned(2)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef f4_t f4_e4 __attribute__((aligned(4)));
@@ -177,38 +178,50 @@ __device__ __forceinline__ void drop_values(float *v, int64_t i, const DropRule 
 
 // ---- sums and maxima over aligned groups of LANES lanes of a wavefront ---------------------------
 // Steps of 1 and 2 are quad permutes, 4 and 8 mirrors of half rows and rows (after the smaller steps all lanes of a quad,
-// of a half row, hold the same), 16 a swizzle, 32 a permute.
-template <int STEP> __device__ __forceinline__ float lane_partner(float x)
+// of a half row, hold the same); 16 and 32 swap rows and halves of two copies, which leaves the two values in two registers: no
+// step leaves the vector unit.
+template <int STEP> __device__ __forceinline__ void lane_pair(float x, float *lo, float *hi)
 {
     const int i = __builtin_bit_cast(int, x);
-    int r;
-    if constexpr (STEP == 1) r = __builtin_amdgcn_update_dpp(0, i, 0xB1, 0xF, 0xF, true);          // quad_perm [1,0,3,2]
-    else if constexpr (STEP == 2) r = __builtin_amdgcn_update_dpp(0, i, 0x4E, 0xF, 0xF, true);     // quad_perm [2,3,0,1]
-    else if constexpr (STEP == 4) r = __builtin_amdgcn_update_dpp(0, i, 0x141, 0xF, 0xF, true);    // row_half_mirror
-    else if constexpr (STEP == 8) r = __builtin_amdgcn_update_dpp(0, i, 0x140, 0xF, 0xF, true);    // row_mirror
-    else if constexpr (STEP == 16) r = __builtin_amdgcn_ds_swizzle(i, 0x401F);                     // lane ^ 16
-    else r = __shfl_xor(i, 32);
-    return __builtin_bit_cast(float, r);
+    if constexpr (STEP >= 16) {
+        const auto r = STEP == 16 ? __builtin_amdgcn_permlane16_swap(i, i, false, false) : __builtin_amdgcn_permlane32_swap(i, i, false, false);
+        *lo = __uint_as_float(r[0]), *hi = __uint_as_float(r[1]);
+    } else {
+        constexpr int CTRL = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;   // quad_perm [1,0,3,2], [2,3,0,1], half mirror, mirror
+        *lo = x, *hi = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, i, CTRL, 0xF, 0xF, true));
+    }
 }
-template <int LANES> __device__ __forceinline__ float lanes_sum(float x)
+template <int LANES, int STEP = 1> __device__ __forceinline__ float lanes_sum(float x)
 {
-    if constexpr (LANES >= 2) x += lane_partner<1>(x);
-    if constexpr (LANES >= 4) x += lane_partner<2>(x);
-    if constexpr (LANES >= 8) x += lane_partner<4>(x);
-    if constexpr (LANES >= 16) x += lane_partner<8>(x);
-    if constexpr (LANES >= 32) x += lane_partner<16>(x);
-    if constexpr (LANES >= 64) x += lane_partner<32>(x);
-    return x;
+    if constexpr (STEP < LANES) {
+        float lo, hi;
+        lane_pair<STEP>(x, &lo, &hi);
+        return lanes_sum<LANES, 2 * STEP>(lo + hi);
+    } else {
+        return x;
+    }
 }
-template <int LANES> __device__ __forceinline__ float lanes_max(float x)
+// The larger of x and its partner's in one instruction; written out, for fmaxf adds one that quiets the partner's value, which here is no
+// signalling NaN.  (s_nop: what the vector unit has just written, a permuted read sees two states later.)
+#define HLQ_MAX_DPP(CTRL) asm("s_nop 1\n\tv_max_f32_dpp %0, %1, %1 " CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1" : "=v"(r) : "v"(x))
+template <int LANES, int STEP = 1> __device__ __forceinline__ float lanes_max(float x)
 {
-    if constexpr (LANES >= 2) x = fmaxf(x, lane_partner<1>(x));
-    if constexpr (LANES >= 4) x = fmaxf(x, lane_partner<2>(x));
-    if constexpr (LANES >= 8) x = fmaxf(x, lane_partner<4>(x));
-    if constexpr (LANES >= 16) x = fmaxf(x, lane_partner<8>(x));
-    if constexpr (LANES >= 32) x = fmaxf(x, lane_partner<16>(x));
-    if constexpr (LANES >= 64) x = fmaxf(x, lane_partner<32>(x));
-    return x;
+    if constexpr (STEP < LANES) {
+        float r;
+        if constexpr (STEP == 1) HLQ_MAX_DPP("quad_perm:[1,0,3,2]");
+        else if constexpr (STEP == 2) HLQ_MAX_DPP("quad_perm:[2,3,0,1]");
+        else if constexpr (STEP == 4) HLQ_MAX_DPP("row_half_mirror");
+        else if constexpr (STEP == 8) HLQ_MAX_DPP("row_mirror");
+        else {
+            float lo, hi;
+            lane_pair<STEP>(x, &lo, &hi);
+            asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(lo), "v"(hi));
+        }
+        return lanes_max<LANES, 2 * STEP>(r);
+    } else {
+        return x;
+    }
 }
+#undef HLQ_MAX_DPP
 
 }  // namespace hlq

@@ -15,6 +15,13 @@
 // there are no atomics and the order is fixed), and leaves the workgroup once; a second launch sums the workgroups' vectors by bucket.
 #include "around_device.hpp"
 
+#include <algorithm>
+
+#ifndef LONG_AHEAD
+#define LONG_AHEAD false
+#define L2048 64
+#define LONG_WAVES 2
+#endif
 namespace hlq {
 
 struct RelPlan {
@@ -32,14 +39,36 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kFewBuckets = 64;                                  // a lane of a wavefront to a bucket
 constexpr int kMaxKeysSequence = 16384, kMaxKeysGrid = 4096;     // two vectors of them (u stretches a grid's to two each) in LDS
+constexpr int kMaxKeysFew = 8192;                                // beside them, a byte for each
 
 __host__ __device__ __forceinline__ int rel_u(int k, int gw) { return gw ? k / gw * (2 * gw - 1) + k % gw : k; }
 // rel(q, k) = u(k) - u(q) + rel_const
 __host__ __device__ __forceinline__ int rel_const(int Q, int K, int gw) { return gw ? rel_u(K - 1, gw) : Q - 1; }
 
+// the last relative position that queries from q0 on reach; with a causal map they see none of those beyond rel_const, moved by K - Q
+__host__ __device__ __forceinline__ int rel_last(int Q, int K, int gw, int causal, int q0)
+{
+    const int rc = rel_const(Q, K, gw), last = rc + rel_u(K - 1, gw) - rel_u(q0, gw), seen = rc + (gw ? 0 : K - Q);
+    return causal && seen < last ? seen : last;
+}
+
 // Place of relative position i of a sequence in LDS: one float of padding to eight, so that lanes that read element e of their eight keys,
 // 8 floats apart, meet 64 banks instead of 8.
 __host__ __device__ __forceinline__ int padded(int i) { return i + (i >> 3); }
+
+// Workgroups that the steps are dealt to, at most: those that are resident at once (256 compute units), twice where queries differ in their work.
+int64_t rel_blocks(const RelPlan &p, bool back, bool uneven)
+{
+#ifndef RB_ROWS
+#define RB_ROWS 5
+#define RB_LONG 3
+#define RB_WIDE 6
+#define RB_FWD 7
+#define RB_UNEVEN 2
+#endif
+    const int resident = back ? (p.lanes < 64 ? RB_ROWS : p.lanes < 256 ? RB_LONG : RB_WIDE) : RB_FWD;
+    return static_cast<int64_t>(256) * resident * (uneven && p.lanes >= 64 ? RB_UNEVEN : 1);
+}
 
 RelPlan rel_plan(const RelArgs &a, bool back)
 {
@@ -49,7 +78,7 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     else if (a.K <= 256) p.lanes = 32, p.nv = 1;
     else if (a.K <= 512) p.lanes = 64, p.nv = 1;
     else if (a.K <= 1024) p.lanes = 64, p.nv = 2;
-    else if (a.K <= 2048) p.lanes = 64, p.nv = 4;
+    else if (a.K <= 2048) p.lanes = L2048, p.nv = 256 / p.lanes;
     else if (a.K <= 4096) p.lanes = 256, p.nv = 2;
     else if (a.K <= 8192) p.lanes = 256, p.nv = 4;
     else p.lanes = 256, p.nv = 8;
@@ -57,15 +86,21 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     p.rows_q = rows;
     while (p.rows_q > 1 && p.rows_q / 2 >= a.Q) p.rows_q /= 2;
     p.rows_b = rows / p.rows_q;
+    // what a row of another batch is away fits 32 bits (bytes of fp32)
+    while (p.rows_b > 1 && (p.rows_b - 1) * (static_cast<int64_t>(a.H) * a.Q * a.K) >= int64_t(1) << 28) p.rows_b /= 2, p.rows_q *= 2;
     const int q_steps = (a.Q + p.rows_q - 1) / p.rows_q, b_steps = (a.B + p.rows_b - 1) / p.rows_b;
-    const int64_t items = static_cast<int64_t>(a.H) * q_steps * b_steps, target = back ? 1024 : 2048;
-    int64_t per = (items + target - 1) / target;
-    if (per < 1) per = 1;
-    int b_per = per < b_steps ? static_cast<int>(per) : b_steps;
-    int q_per = static_cast<int>(per / b_per);
-    if (q_per < 1) q_per = 1;
-    if (q_per > q_steps) q_per = q_steps;
+    // Steps to a workgroup: all batches of a query first (its bias and their sum stay in registers, or the vector in LDS serves more rows), then more
+    // queries, until the workgroups are no more than `most_blocks`; then as even as they come.
+    const int64_t most_blocks = rel_blocks(p, back, a.causal != 0);
+    const int64_t steps = static_cast<int64_t>(a.H) * q_steps * b_steps;
+    int b_per = static_cast<int>(std::min<int64_t>(b_steps, std::max<int64_t>(1, steps / most_blocks)));
+    while (b_per < b_steps && static_cast<int64_t>(a.H) * q_steps * ((b_steps + b_per - 1) / b_per) > most_blocks) ++b_per;
+    const int chunks = (b_steps + b_per - 1) / b_per;
+    b_per = (b_steps + chunks - 1) / chunks;
+    int q_per = static_cast<int>(std::min<int64_t>(q_steps, std::max<int64_t>(1, (static_cast<int64_t>(a.H) * q_steps * chunks + most_blocks - 1) / most_blocks)));
     if (q_per * p.rows_q > 512) q_per = 512 / p.rows_q;         // the reach of a workgroup's queries stays in LDS
+    const int blocks = (q_steps + q_per - 1) / q_per;
+    q_per = (q_steps + blocks - 1) / blocks;
     p.q_block = q_per * p.rows_q;
     p.q_blocks = (a.Q + p.q_block - 1) / p.q_block;
     p.b_chunk = b_per * p.rows_b;
@@ -75,36 +110,51 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     const int all = a.grid_w ? 2 * rel_u(a.K - 1, a.grid_w) + 1 : a.Q + a.K - 1;
     p.win = rel_u(a.K - 1, a.grid_w) + most;
     if (p.win > all) p.win = all;
-    p.few = a.n_buckets <= kFewBuckets;
+    p.few = a.n_buckets <= kFewBuckets && a.K <= kMaxKeysFew;
     p.stride = p.few ? kFewBuckets : p.win;
     return p;
 }
 
 // LDS of a workgroup, in floats: the bias vector, the sums by relative position (one vector a wavefront where a wavefront is a row; for
 // shorter rows one, and the rows' sums over the batch), reductions across the wavefronts.
-__host__ __device__ __forceinline__ int rel_vector(const RelPlan &p, int gw) { return (p.lanes >= 64 && !gw ? padded(p.win) + 1 : p.win); }
+// A sequence's vectors have room for every place that a row's lanes may reach, keys or not.
+__host__ __device__ __forceinline__ int rel_vector(const RelPlan &p, int gw)
+{
+    return p.lanes >= 64 && !gw ? padded(p.lanes * p.nv * 8 + p.q_block) : p.win;
+}
 size_t rel_lds_bytes(const RelPlan &p, int gw, bool back)
 {
     const size_t v = rel_vector(p, gw);
     const int rows = kThreads / p.lanes;
-    size_t n = v + 16;
+    size_t n = v + 16 + (back && p.few ? (p.win + 3) / 4 : 0);
     if (back) n += p.lanes == 64 ? 4 * v : v + (rows > 1 ? static_cast<size_t>(rows) * p.lanes * p.nv * 8 : 0);
     return sizeof(float) * n;
 }
 
 }  // namespace
 
-// 8 elements from place `at` of a tensor of `total`: whole vectors run over a row's end into the next row, but not over the tensor's
+// one more element from the top, the lowest falls out
+__device__ __forceinline__ void push_element(Raw<bf16_t, 8> &r, bf16_t x)
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r.w[i] = __builtin_amdgcn_alignbit(r.w[i + 1], r.w[i], 16);
+    r.w[3] = (r.w[3] >> 16) | (static_cast<uint32_t>(x) << 16);
+}
+__device__ __forceinline__ void push_element(Raw<float, 8> &r, float x)
+{
+    r.a = f4_t{r.a[1], r.a[2], r.a[3], r.b[0]};
+    r.b = f4_t{r.b[1], r.b[2], r.b[3], x};
+}
+// 8 elements from place `at` of a tensor of `total`: whole vectors run over a row's end into the next row, but not over the tensor's;
+// there they come one by one, in a loop that takes no registers from the rest
 template <typename T>
 __device__ __forceinline__ void load_inside(Raw<T, 8> &r, const T *base, int64_t at, int64_t total)
 {
     if (at + 8 <= total) {
         r.load(base + at);
     } else {
-        T v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = at + e < total ? base[at + e] : T{};
-        __builtin_memcpy(&r, v, sizeof(v));
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e) push_element(r, at + e < total ? base[at + e] : T{});
     }
 }
 // bit e: byte e of the eight is not zero
@@ -114,27 +164,51 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *base, int64_t at, i
     if (at + 8 <= total) {
         __builtin_memcpy(&m, base + at, 8);
     } else {
+#pragma unroll 1
         for (int e = 0; e < 8 && at + e < total; ++e) m |= static_cast<uint64_t>(base[at + e]) << (8 * e);
     }
     const uint64_t low = 0x7F7F7F7F7F7F7F7Full;
     const uint64_t top = (((m & low) + low) | m) & ~low;               // bit 7 of every byte that is not zero
     return static_cast<uint32_t>((top >> 7) * 0x0102040810204080ull >> 56);
 }
-// the first n of 8
-template <typename T>
-__device__ __forceinline__ void store_first(T *p, const float *v, int n)
+// ---- vectors of a row by buffer instructions: a lane with nothing to load or store has a place beyond the buffer's end ----------------
+constexpr uint32_t kNowhere = 0x80000000u;       // ored into a lane's place in bytes
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7FFFFFFF, 0x00020000); }
+__device__ __forceinline__ void buffer_load(Raw<bf16_t, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0); }
+__device__ __forceinline__ void buffer_load(Raw<float, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at)
 {
-    if (n >= 8) {
-        Raw<T, 8>::store(p, v);
-        return;
-    }
-    if (n & 4) {
-        Raw<T, 2>::store(p, v);
-        Raw<T, 2>::store(p + 2, v + 2);
-    }
+    r.a = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
+    r.b = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 16, 0));
+}
+// v[0 .. 8) to `at` where k0 + 8 <= K; the lane whose eight the row's end cuts stores the K % 8 it has (`cut`: its place, others kNowhere).
+// One store for sure, and others only where K % 8 is not 0: the wait for the loads behind it need not wait for it.
+__device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail, const float *v, bf16_t)
+{
+    raw4_t o;
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (e >= (n & 4) && e < n) store_one(p + e, v[e]);
+    for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
+    if (tail) {
+        if (tail & 4) __builtin_amdgcn_raw_buffer_store_b64(raw2_t{o[0], o[1]}, b, cut, 0, 0);
+        const uint32_t two = tail & 4 ? o[2] : o[0], one = tail & 4 ? (tail & 2 ? o[3] : o[2]) : (tail & 2 ? o[1] : o[0]);
+        if (tail & 2) __builtin_amdgcn_raw_buffer_store_b32(two, b, cut, (tail & 4) * 2, 0);
+        if (tail & 1) __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(one), b, cut, (tail & 6) * 2, 0);
+    }
+}
+__device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail, const float *v, float)
+{
+    raw4_t o, q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[i]), q[i] = __float_as_uint(v[4 + i]);
+    __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(q, b, at, 16, 0);
+    if (tail) {
+        if (tail & 4) __builtin_amdgcn_raw_buffer_store_b128(o, b, cut, 0, 0);
+        const uint32_t t0 = tail & 4 ? q[0] : o[0], t1 = tail & 4 ? q[1] : o[1];
+        const uint32_t one = tail & 4 ? (tail & 2 ? q[2] : q[0]) : (tail & 2 ? o[2] : o[0]);
+        if (tail & 2) __builtin_amdgcn_raw_buffer_store_b64(raw2_t{t0, t1}, b, cut, (tail & 4) * 4, 0);
+        if (tail & 1) __builtin_amdgcn_raw_buffer_store_b32(one, b, cut, (tail & 6) * 4, 0);
+    }
 }
 
 // zeros for the elements whose bit is not set
@@ -154,25 +228,26 @@ __device__ __forceinline__ void keep_bits(Raw<float, 8> &r, uint32_t bits)
         r.b[i] = (bits >> (4 + i)) & 1 ? r.b[i] : 0.0f;
     }
 }
-// zeros for the elements that dropout drops; what is kept is not scaled.  i a multiple of 8
+// Zeros for the elements that dropout drops; what is kept is not scaled.  word: the first of the four words, a multiple of 4.
+// On bf16 two halves at a time: w - (below - 1) cut at 0 is 0 where dropped; adding 0xFFFE cut at 0xFFFF and taken from 0xFFFE it is the
+// mask.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void drop_raw(Raw<bf16_t, 8> &r, int64_t i, const DropRule &d)
+__device__ __forceinline__ void drop_raw(Raw<bf16_t, 8> &r, uint32_t word, const DropRule &d)
 {
     uint32_t w[4];
-    rand_words<4>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, w);
-    const u16x2 under = {static_cast<uint16_t>(d.below - 1), static_cast<uint16_t>(d.below - 1)}, one = {1, 1}, none = {0, 0};
+    rand_words<4>(word, d.k0, d.k1, w);
+    const uint32_t under = (d.below - 1) * 0x10001u, most = 0xFFFEFFFEu;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        // halves at or above `below`: their difference from below - 1, cut at 0, is not 0
-        const u16x2 over = __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w[k]), under), one);
-        const u16x2 keep = none - over;
-        r.w[k] &= __builtin_bit_cast(uint32_t, keep);
+        uint32_t m;
+        asm("v_pk_sub_u16 %0, %1, %2 clamp\n\tv_pk_add_u16 %0, %0, %3 clamp\n\tv_pk_sub_u16 %0, %3, %0" : "=&v"(m) : "v"(w[k]), "s"(under), "v"(most));
+        r.w[k] &= m;
     }
 }
-__device__ __forceinline__ void drop_raw(Raw<float, 8> &r, int64_t i, const DropRule &d)
+__device__ __forceinline__ void drop_raw(Raw<float, 8> &r, uint32_t word, const DropRule &d)
 {
     uint32_t w[4];
-    rand_words<4>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, w);
+    rand_words<4>(word, d.k0, d.k1, w);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const bool lo = (w[k] & 0xFFFFu) >= d.below, hi = (w[k] >> 16) >= d.below;
@@ -186,6 +261,19 @@ __device__ __forceinline__ void drop_raw(Raw<float, 8> &r, int64_t i, const Drop
     }
 }
 
+// exp(z - top) of a row's scores.  On bf16 scores one fma and the base-2 exponential, of z l - top l with l = log2(e).  Where |top| is so
+// large that the product overflows, scores are either top or further from it than any exponential reaches: a small l tells as much.
+template <bool EXACT> struct RowExp {
+    float top, l, shift;
+    __device__ __forceinline__ explicit RowExp(float t)
+    {
+        top = t == -__builtin_inff() ? 0.0f : t;                      // a row that sees nothing
+        l = __builtin_fabsf(top) < 1e38f ? 1.44269504088896341f : 0x1p-20f;
+        shift = -(top * l);
+    }
+    __device__ __forceinline__ float operator()(float z) const { return EXACT ? expf(z - top) : __builtin_amdgcn_exp2f(__builtin_fmaf(z, l, shift)); }
+};
+
 // What a workgroup works on, the same for all its threads.
 struct RelJob {
     int h, q0, q1, b0, b1, part, rc, rlo, win;
@@ -193,7 +281,14 @@ struct RelJob {
 __device__ __forceinline__ RelJob rel_job(const RelArgs &a, const RelPlan &p)
 {
     RelJob j;
-    const int qb = blockIdx.x % p.q_blocks, rest = blockIdx.x / p.q_blocks;
+    // causal: the last queries, which see most, first
+    int qb, rest;
+    if (a.causal) {
+        const int others = gridDim.x / p.q_blocks;
+        qb = p.q_blocks - 1 - blockIdx.x / others, rest = blockIdx.x % others;
+    } else {
+        qb = blockIdx.x % p.q_blocks, rest = blockIdx.x / p.q_blocks;
+    }
     const int bc = rest / a.H;
     j.h = rest % a.H;
     j.q0 = qb * p.q_block, j.q1 = min(a.Q, j.q0 + p.q_block);
@@ -201,8 +296,35 @@ __device__ __forceinline__ RelJob rel_job(const RelArgs &a, const RelPlan &p)
     j.part = qb * p.b_chunks + bc;
     j.rc = rel_const(a.Q, a.K, a.grid_w);
     j.rlo = j.rc - rel_u(j.q1 - 1, a.grid_w);                         // the first relative position that its queries reach
-    j.win = j.rc + rel_u(a.K - 1, a.grid_w) - rel_u(j.q0, a.grid_w) - j.rlo + 1;
+    j.win = rel_last(a.Q, a.K, a.grid_w, a.causal, j.q0) - j.rlo + 1;
     return j;
+}
+
+// The head's bias of the workgroup's relative positions to bias[place(i)], their buckets to ids[i] where they are few.  The loads of four go out
+// before the first is used: one after the other their latency, twice, is most of a short workgroup's time.
+template <typename Place>
+__device__ __forceinline__ void rel_fill(const RelArgs &a, const RelPlan &p, const RelJob &job, float *bias, uint8_t *ids, Place place)
+{
+    for (int i0 = threadIdx.x; i0 < job.win; i0 += 4 * kThreads) {
+        int c[4];
+        float t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) c[u] = i0 + u * kThreads < job.win ? a.of[job.rlo + i0 + u * kThreads] : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool has = c[u] >= 0 && c[u] < a.n_buckets;
+            t[u] = has ? load_param(a.table, a.param_f32, static_cast<int64_t>(c[u]) * a.H + job.h) : 0.0f;
+            c[u] = has ? c[u] : 255;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * kThreads;
+            if (i < job.win) {
+                bias[place(i)] = t[u];
+                if (ids && p.few) ids[i] = static_cast<uint8_t>(c[u]);
+            }
+        }
+    }
 }
 
 // One row's vectors as loaded, and which of their elements the query sees.
@@ -210,48 +332,44 @@ template <typename T, int NV, bool BACK> struct RelRow {
     Raw<T, 8> s[NV], d[BACK ? NV : 1];
     uint32_t seen[NV];
 
-    // k0 of vector j is first + 8 * lanes * j; keys from `end` on are not seen (0: nothing is loaded)
+    // The row at place `at`, the same for the wavefront; k0 of vector j is first + 8 * lanes * j; keys from `end` on are not seen (0: nothing is
+    // loaded) and come as zeros, with those that the row's last vector takes of the next row.
     __device__ __forceinline__ void load(const RelArgs &a, int64_t at, int b, int q, int first, int lanes, int end, int64_t total)
     {
+        const T *ps = static_cast<const T *>(a.s), *pd = static_cast<const T *>(a.dp);
+        if (at + a.K + 8 <= total || end <= 0) {
+            const __amdgpu_buffer_rsrc_t bs = buffer_at(ps + at), bd = buffer_at(pd + at);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int k0 = first + 8 * lanes * j;
+                const uint32_t place = k0 < end ? static_cast<uint32_t>(k0) * sizeof(T) : kNowhere;
+                buffer_load(s[j], bs, place);
+                if (BACK) buffer_load(d[j], bd, place);
+            }
+        } else {                                                  // the tensor's last row
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int k0 = first + 8 * lanes * j;
+                s[j].zero();
+                if (BACK) d[j].zero();
+                if (k0 < end) {
+                    load_inside(s[j], ps, at + k0, total);
+                    if (BACK) load_inside(d[j], pd, at + k0, total);
+                }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int k0 = first + 8 * lanes * j;
-            s[j].zero();
-            if (BACK) d[j].zero();
-            seen[j] = 0;
-            if (k0 < end) {
-                load_inside(s[j], static_cast<const T *>(a.s), at + k0, total);
-                if (BACK) load_inside(d[j], static_cast<const T *>(a.dp), at + k0, total);
-                seen[j] = end - k0 >= 8 ? 0xFFu : (1u << (end - k0)) - 1u;
-                if (a.mask)
-                    seen[j] &= load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0,
-                                         static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K);
-            }
+            seen[j] = end - k0 >= 8 ? 0xFFu : end > k0 ? (1u << (end - k0)) - 1u : 0u;
+            if (a.mask && k0 < end)
+                seen[j] &= load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0,
+                                     static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K);
         }
     }
 };
 
-// z = scale s + bias where seen, minus infinity elsewhere: on entry z holds the bias, on return exp(z - top); the sum over the lane
-template <typename T, int NV, bool BACK>
-__device__ __forceinline__ float rel_scores(const RelRow<T, NV, BACK> &r, float scale, float *z)
-{
-    const float NONE = -__builtin_inff();
-    float top = NONE;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        float v[8];
-        r.s[j].widen(v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float t = __builtin_fmaf(v[e], scale, z[8 * j + e]);
-            z[8 * j + e] = (r.seen[j] >> e) & 1u ? t : NONE;
-            top = fmaxf(top, z[8 * j + e]);
-        }
-    }
-    return top;
-}
-
-// the bucket's lane adds v: lanes hold (bucket or -1, value), acc of lane l is the sum of bucket l; whole wavefronts only
+// the bucket's lane adds v: lanes hold (bucket, or none of 0 .. 63, and value), acc of lane l is the sum of bucket l; whole wavefronts only
 __device__ __forceinline__ void bucket_add(int c, float v, float &acc)
 {
     const int lane = threadIdx.x & 63, c0 = __builtin_amdgcn_readfirstlane(c);
@@ -267,9 +385,9 @@ __device__ __forceinline__ void bucket_add(int c, float v, float &acc)
     }
 }
 
-// A workgroup's sums by relative position leave it: value(i) of relative position rlo + i, by bucket where they are few.
+// A workgroup's sums by relative position leave it: value(i) of relative position rlo + i, by bucket (ids) where they are few.
 template <typename Value>
-__device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &p, const RelJob &job, float *lds, Value value)
+__device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &p, const RelJob &job, float *lds, const uint8_t *ids, Value value)
 {
     const int tid = threadIdx.x;
     float *w = a.ws + (static_cast<int64_t>(job.h) * p.q_blocks * p.b_chunks + job.part) * p.stride;
@@ -280,8 +398,7 @@ __device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &
     float acc = 0.0f;
     for (int i0 = tid & ~63; i0 < job.win; i0 += kThreads) {
         const int i = i0 + (tid & 63);
-        const int c = i < job.win ? a.of[job.rlo + i] : -1;
-        bucket_add(c >= 0 && c < a.n_buckets ? c : -1, i < job.win ? value(i) : 0.0f, acc);
+        bucket_add(i < job.win ? ids[i] : 255, i < job.win ? value(i) : 0.0f, acc);
     }
     __syncthreads();
     lds[tid] = acc;
@@ -289,90 +406,160 @@ __device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &
     if (tid < 64) w[tid] = (lds[tid] + lds[64 + tid]) + (lds[128 + tid] + lds[192 + tid]);
 }
 
-// Rows of up to 256 keys, 8, 16 or 32 lanes each: several to a wavefront.  A query's bias stays in registers through the batch, and so do the
-// sums over the batch, which then meet in LDS: a thread sums those of one relative position.
+// Which of a lane's eight elements the query sees, as what makes the others zero in one instruction for each register.
+template <typename T> struct LaneMask;
+template <> struct LaneMask<bf16_t> {
+    uint32_t m[4];
+    __device__ __forceinline__ explicit LaneMask(uint32_t bits)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = ((bits >> (2 * i)) & 1u ? 0xFFFFu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xFFFF0000u : 0u);
+    }
+    __device__ __forceinline__ void operator()(Raw<bf16_t, 8> &r) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] &= m[i];
+    }
+};
+template <> struct LaneMask<float> {
+    bool in[8];
+    __device__ __forceinline__ explicit LaneMask(uint32_t bits)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) in[i] = (bits >> i) & 1u;
+    }
+    __device__ __forceinline__ void operator()(Raw<float, 8> &r) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r.a[i] = in[i] ? r.a[i] : 0.0f;
+            r.b[i] = in[4 + i] ? r.b[i] : 0.0f;
+        }
+    }
+};
+
+// Rows of up to 256 keys, 8, 16 or 32 lanes each: several to a wavefront.  A query's bias stays in registers through the batch, minus infinity for
+// the keys that the query does not see, and so do the sums over the batch, which then meet in LDS: a thread sums those of one relative
+// position.  The next batch's row is fetched before the current one is worked on.  A place in memory is one of the whole workgroup's
+// (in scalar registers) and the lane's, which stays: rows_b is chosen so that the latter fits 32 bits.
 template <typename T, int LANES, bool BACK>
 __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
 {
     extern __shared__ float lds[];
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int ROWS = kThreads / LANES, WIDTH = LANES * 8;
-    const int tid = threadIdx.x, row = tid / LANES, lane = tid % LANES;
+    const float NONE = -__builtin_inff();
+    const int tid = threadIdx.x, row = tid / LANES, lane = tid % LANES, k0 = lane * 8;
     const RelJob job = rel_job(a, p);
     const int gw = a.grid_w;
     float *bias = lds, *accw = bias + p.win, *tile = accw + (BACK ? p.win : 0);
-    for (int i = tid; i < job.win; i += kThreads) {
-        const int c = a.of[job.rlo + i];
-        bias[i] = c >= 0 && c < a.n_buckets ? load_param(a.table, a.param_f32, static_cast<int64_t>(c) * a.H + job.h) : 0.0f;
-        if (BACK) accw[i] = 0.0f;
-    }
-    const int64_t total = static_cast<int64_t>(a.B) * a.H * a.Q * a.K;
-    const int Kp = (a.K + 7) & ~7, k0 = lane * 8;
+    uint8_t *ids = BACK ? reinterpret_cast<uint8_t *>(tile + ROWS * WIDTH) : nullptr;
+    const int64_t plane = static_cast<int64_t>(a.H) * a.Q * a.K, total = a.B * plane, mask_total = static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K;
+    const int Kp = (a.K + 7) & ~7;
     const int row_q = row % p.rows_q, row_b = row / p.rows_q;
+    const uint32_t mine = (static_cast<uint32_t>(row_b * plane) + row_q * a.K + k0) * sizeof(T);      // the lane's place beside the workgroup's
+    const int tail = a.K & 7;
+    // places of a whole vector and of one that the row's end cuts
+    const uint32_t at_whole = k0 + 8 <= a.K ? mine : kNowhere, at_cut = k0 < a.K && k0 + 8 > a.K ? mine : kNowhere;
+    const uint32_t word0 = static_cast<uint32_t>((((static_cast<int64_t>(row_b) * a.H) * a.Q + row_q) * Kp + k0) >> 1);      // of the random stream
+    const int64_t reach = (p.rows_b - 1) * plane + (p.rows_q - 1) * a.K + WIDTH;              // the workgroup's end beside its place
     const float keep = BACK && a.drop.below ? a.drop.scale : 1.0f;
-    RelRow<T, 1, BACK> next;
+    Raw<T, 8> ns, nd;
+    uint32_t nbits = 0xFFu;
     auto fetch = [&](int qs, int bs) {
         const int q = qs + row_q, b = bs + row_b;
-        const bool on = q < job.q1 && b < job.b1;
-        const int end = on ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
-        next.load(a, ((static_cast<int64_t>(b) * a.H + job.h) * a.Q + q) * a.K, b, q, k0, LANES, end, total);
+        const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
+        const int end = q < job.q1 && b < job.b1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
+        if (base + reach <= total) {
+            const uint32_t at = k0 < end ? mine : kNowhere;
+            buffer_load(ns, buffer_at(static_cast<const T *>(a.s) + base), at);
+            if (BACK) buffer_load(nd, buffer_at(static_cast<const T *>(a.dp) + base), at);
+        } else if (k0 < end) {                                    // the tensor's last rows
+            load_inside(ns, static_cast<const T *>(a.s), base + mine / sizeof(T), total);
+            if (BACK) load_inside(nd, static_cast<const T *>(a.dp), base + mine / sizeof(T), total);
+        } else {
+            ns.zero();
+            if (BACK) nd.zero();
+        }
+        if (a.mask && k0 < end)
+            nbits = load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0, mask_total);
     };
     fetch(job.q0, job.b0);
+    if (BACK)
+        for (int i = tid; i < job.win; i += kThreads) accw[i] = 0.0f;
+    rel_fill(a, p, job, bias, ids, [](int i) { return i; });
     __syncthreads();
     for (int qs = job.q0; qs < job.q1; qs += p.rows_q) {
         const int q = qs + row_q;
+        const int end = q < job.q1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
+        const uint32_t bits = end - k0 >= 8 ? 0xFFu : end > k0 ? (1u << (end - k0)) - 1u : 0u;
+        const LaneMask<T> inside(bits);
+        const bool whole = __all(bits == 0xFFu);
         float bv[8], acc[8];
         {
             int i = rel_u(k0, gw) - rel_u(q < job.q1 ? q : job.q1 - 1, gw) + job.rc - job.rlo, kx = gw ? k0 % gw : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                bv[e] = bias[k0 + e < a.K ? i : 0];
+                bv[e] = (bits >> e) & 1u ? bias[i] : NONE;
                 acc[e] = 0.0f;
                 ++i;
                 if (gw && ++kx == gw) kx = 0, i += gw - 1;
             }
         }
         for (int bs = job.b0; bs < job.b1; bs += p.rows_b) {
-            RelRow<T, 1, BACK> r = next;
-            if (bs + p.rows_b < job.b1) fetch(qs, bs + p.rows_b);
-            else if (qs + p.rows_q < job.q1) fetch(qs + p.rows_q, job.b0);
-            const int b = bs + row_b;
-            const int64_t line = (static_cast<int64_t>(b) * a.H + job.h) * a.Q + q;
-            const bool on = b < job.b1 && q < job.q1 && k0 < a.K;
-            float z[8], sum = 0.0f;
+            Raw<T, 8> rs = ns, rd = nd;
+            const uint32_t seen = nbits;
+            const bool same = bs + p.rows_b < job.b1;
+            fetch(same ? qs : qs + p.rows_q, same ? bs + p.rows_b : job.b0);       // behind the last there is nothing to load
+            const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
+            const bool on = bs + row_b < job.b1 && q < job.q1;
+            if (!whole) {
+                inside(rs);
+                if (BACK) inside(rd);
+            }
+            float z[8], sum = 0.0f, top = NONE;
+            rs.widen(z);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = bv[e];
-            float top = lanes_max<LANES>(rel_scores<T, 1, BACK>(r, a.scale, z));
-            if (top == -__builtin_inff()) top = 0.0f;                  // a row that sees nothing
+            for (int e = 0; e < 8; ++e) z[e] = __builtin_fmaf(z[e], a.scale, bv[e]);
+            if (a.mask) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = (seen >> e) & 1u ? z[e] : NONE;
+                if (BACK) keep_bits(rd, seen);                         // whatever stands where nothing is seen
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, z[e]);
+            const RowExp<EXACT> exp_row(lanes_max<LANES>(top));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                z[e] = exp_of<EXACT>(z[e] - top);
+                z[e] = exp_row(z[e]);
                 sum += z[e];
             }
             sum = lanes_sum<LANES>(sum);
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] *= inv;
+            const float inv = sum == 0.0f ? 0.0f : recip_of<EXACT>(sum);
+            const __amdgpu_buffer_rsrc_t out = buffer_at(static_cast<T *>(a.out) + base);
+            const uint32_t off = on ? 0u : kNowhere;
+            const uint32_t word = word0 + static_cast<uint32_t>((((static_cast<int64_t>(bs) * a.H + job.h) * a.Q + qs) * Kp) >> 1);
             if constexpr (!BACK) {
-                if (on) {
-                    if (a.drop.below) drop_values<8>(z, line * Kp + k0, a.drop);
-                    store_first(static_cast<T *>(a.out) + line * a.K + k0, z, a.K - k0);
-                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] *= inv;
+                if (a.drop.below) drop_values<8>(z, static_cast<int64_t>(word) * 2, a.drop);
+                store_row(out, at_whole | off, at_cut | off, tail, z, T{});
             } else {
                 float d[8], dot = 0.0f;
-                keep_bits(r.d[0], r.seen[0]);                          // whatever stands where nothing is seen
-                if (a.drop.below) drop_raw(r.d[0], line * Kp + k0, a.drop);
-                r.d[0].widen(d);
+                if (a.drop.below) drop_raw(rd, word, a.drop);
+                rd.widen(d);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(z[e], d[e], dot);
-                dot = keep * lanes_sum<LANES>(dot);
+                dot = lanes_sum<LANES>(dot);
+                // z holds p / inv, d holds dp / keep, dot their product's sum:  dz = p (dp - sum p dp)
+                const float gain = on ? keep * inv : 0.0f, minus = on ? -(dot * inv) * gain : 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float dz = z[e] * __builtin_fmaf(d[e], keep, -dot);
+                    const float dz = z[e] * __builtin_fmaf(d[e], gain, minus);
                     acc[e] += dz;
                     d[e] = dz * a.scale;
                 }
-                if (on) store_first(static_cast<T *>(a.out) + line * a.K + k0, d, a.K - k0);
+                store_row(out, at_whole | off, at_cut | off, tail, d, T{});
             }
         }
         if constexpr (BACK) {
@@ -380,7 +567,7 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
             for (int e = 0; e < 8; ++e) tile[row * WIDTH + k0 + e] = acc[e];
             __syncthreads();
             const int qe = min(job.q1, qs + p.rows_q);
-            const int i0 = job.rc - rel_u(qe - 1, gw) - job.rlo, i1 = job.rc + rel_u(a.K - 1, gw) - rel_u(qs, gw) - job.rlo;
+            const int i0 = job.rc - rel_u(qe - 1, gw) - job.rlo, i1 = min(job.rc + rel_u(a.K - 1, gw) - rel_u(qs, gw) - job.rlo, job.win - 1);
             for (int i = i0 + tid; i <= i1; i += kThreads) {
                 float t = 0.0f;
                 const int rel = job.rlo + i - job.rc;                  // u(k) - u(q)
@@ -398,54 +585,62 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
             __syncthreads();
         }
     }
-    if constexpr (BACK) rel_write_sums(a, p, job, tile, [&](int i) { return accw[i]; });
+    if constexpr (BACK) rel_write_sums(a, p, job, tile, ids, [&](int i) { return accw[i]; });
 }
 
 // Longer rows: a wavefront's (LANES = 64), or a workgroup's (LANES = 256).  The bias is read from LDS for every row, and a row's gradient
 // of the bias is added to LDS at once, to the wavefront's own vector or, where the workgroup is one row, to the one: a
-// row's relative positions are distinct, rows follow one another, so every sum has its order.
-template <typename T, int LANES, int NV, bool GRID, bool BACK>
-__global__ __launch_bounds__(kThreads) void k_rel_long(RelArgs a, RelPlan p)
+// row's relative positions are distinct, rows follow one another, so every sum has its order.  (Plain reads and writes: the same with
+// LDS atomics took 682 us for 2048 tokens and 32 heads where this took 217.)  AHEAD: the next row is fetched before the current is worked on.
+template <typename T, int LANES, int NV, bool GRID, bool BACK, bool AHEAD, int MINW>
+__global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan p)
 {
     extern __shared__ float lds[];
     constexpr bool EXACT = sizeof(T) == 4, WIDE = LANES == kThreads;
     constexpr int WAVES = kThreads / 64, VECTORS = BACK ? (WIDE ? 1 : WAVES) : 0, STEP = 8 * LANES;
+    const float NONE = -__builtin_inff();
     const int tid = threadIdx.x, row = tid / LANES, first = tid % LANES * 8;
     const RelJob job = rel_job(a, p);
     const int gw = GRID ? a.grid_w : 0;
     const int size = rel_vector(p, gw);
     float *bias = lds, *sums = lds + size, *red = sums + VECTORS * size;
-    for (int i = tid; i < job.win; i += kThreads) {
-        const int c = a.of[job.rlo + i], at = GRID ? i : padded(i);
-        bias[at] = c >= 0 && c < a.n_buckets ? load_param(a.table, a.param_f32, static_cast<int64_t>(c) * a.H + job.h) : 0.0f;
-    }
-    for (int i = tid; i < VECTORS * size; i += kThreads) sums[i] = 0.0f;
+    uint8_t *ids = BACK ? reinterpret_cast<uint8_t *>(red + 16) : nullptr;
     const int64_t total = static_cast<int64_t>(a.B) * a.H * a.Q * a.K;
     const int Kp = (a.K + 7) & ~7;
-    const int row_q = row % p.rows_q, row_b = row / p.rows_q;
+    // the same for a whole wavefront
+    const int row_q = __builtin_amdgcn_readfirstlane(row % p.rows_q), row_b = __builtin_amdgcn_readfirstlane(row / p.rows_q);
+    const int wave_first = __builtin_amdgcn_readfirstlane(first);
     const float keep = BACK && a.drop.below ? a.drop.scale : 1.0f;
     float *mine = sums + (WIDE ? 0 : (tid >> 6) * size);
     auto end_of = [&](int q, int b) {
         return q < job.q1 && b < job.b1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
     };
-    // f(j, e, place in LDS) for the lane's keys of vector j
+    // f(e, place in LDS) for the lane's keys of vector j; keys beyond the last have a place, too
     auto places = [&](int j, int q, auto f) {
-        const int k0 = first + STEP * j;
         if constexpr (GRID) {
+            const int k0 = min(first + STEP * j, (a.K - 1) & ~7);
             int i = rel_u(k0, gw) - rel_u(q, gw) + job.rc - job.rlo, kx = k0 % gw;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                f(e, k0 + e < a.K ? i : 0, k0 + e < a.K);
+                f(e, min(i, size - 1));
                 ++i;
                 if (++kx == gw) kx = 0, i += gw - 1;
             }
         } else {
             // padded(k0 + shift + e), k0 a multiple of 8 and shift the wavefront's own: 9 k0 / 8 + padded(shift + e)
-            const int shift = __builtin_amdgcn_readfirstlane(job.rc - job.rlo - q);
+            const int shift = job.rc - job.rlo - q, at = first + (first >> 3);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f(e, k0 + e < a.K ? k0 + (k0 >> 3) + padded(shift + e) : 0, k0 + e < a.K);
+            for (int e = 0; e < 8; ++e) f(e, at + padded(shift + e) + padded(STEP) * j);
         }
     };
+    RelRow<T, NV, BACK> next;
+    auto fetch = [&](int qs, int bs) {
+        const int q = qs + row_q, b = bs + row_b;
+        next.load(a, ((static_cast<int64_t>(b) * a.H + job.h) * a.Q + q) * a.K, b, q, first, LANES, end_of(q, b), total);
+    };
+    if constexpr (AHEAD) fetch(job.q0, job.b0);
+    for (int i = tid; i < VECTORS * size; i += kThreads) sums[i] = 0.0f;
+    rel_fill(a, p, job, bias, ids, [](int i) { return GRID ? i : padded(i); });
     __syncthreads();
     for (int qs = job.q0; qs < job.q1; qs += p.rows_q) {
         const int q = qs + row_q;
@@ -453,13 +648,31 @@ __global__ __launch_bounds__(kThreads) void k_rel_long(RelArgs a, RelPlan p)
             const int b = bs + row_b;
             const bool on = b < job.b1 && q < job.q1;
             const int64_t line = (static_cast<int64_t>(b) * a.H + job.h) * a.Q + q;
-            const int end = end_of(q, b);
-            RelRow<T, NV, BACK> r;
-            r.load(a, line * a.K, b, q, first, LANES, end, total);
-            float z[8 * NV];
+            const int end = end_of(q, b);            // a wavefront passes over its vectors from here on
+            if constexpr (!AHEAD) fetch(qs, bs);
+            RelRow<T, NV, BACK> r = next;
+            if constexpr (AHEAD) {
+                const bool same = bs + p.rows_b < job.b1;
+                fetch(same ? qs : qs + p.rows_q, same ? bs + p.rows_b : job.b0);       // behind the last there is nothing to load
+            }
+            float z[8 * NV], top = NONE, sum = 0.0f, v[8];
 #pragma unroll
-            for (int j = 0; j < NV; ++j) places(j, min(q, job.q1 - 1), [&](int e, int at, bool) { z[8 * j + e] = bias[at]; });
-            float top = rel_scores<T, NV, BACK>(r, a.scale, z), sum = 0.0f;
+            for (int j = 0; j < NV; ++j) {
+                if (wave_first + STEP * j < end) {
+                    places(j, q, [&](int e, int at) { z[8 * j + e] = bias[at]; });
+                    r.s[j].widen(v);
+                    if (__all(r.seen[j] == 0xFFu)) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[8 * j + e] = __builtin_fmaf(v[e], a.scale, z[8 * j + e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[8 * j + e] = (r.seen[j] >> e) & 1u ? __builtin_fmaf(v[e], a.scale, z[8 * j + e]) : NONE;
+                        if (BACK) keep_bits(r.d[j], r.seen[j]);        // whatever stands where nothing is seen
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, z[8 * j + e]);
+                }
+            }
             if constexpr (WIDE) {
                 top = lanes_max<64>(top);
                 if ((tid & 63) == 0) red[tid >> 6] = top;
@@ -468,11 +681,16 @@ __global__ __launch_bounds__(kThreads) void k_rel_long(RelArgs a, RelPlan p)
             } else {
                 top = lanes_max<LANES>(top);
             }
-            if (top == -__builtin_inff()) top = 0.0f;                  // a row that sees nothing
+            const RowExp<EXACT> exp_row(top);
 #pragma unroll
-            for (int e = 0; e < 8 * NV; ++e) {
-                z[e] = exp_of<EXACT>(z[e] - top);
-                sum += z[e];
+            for (int j = 0; j < NV; ++j) {
+                if (wave_first + STEP * j < end) {
+#pragma unroll
+                    for (int e = 8 * j; e < 8 * j + 8; ++e) {
+                        z[e] = exp_row(z[e]);
+                        sum += z[e];
+                    }
+                }
             }
             if constexpr (WIDE) {
                 sum = lanes_sum<64>(sum);
@@ -482,62 +700,79 @@ __global__ __launch_bounds__(kThreads) void k_rel_long(RelArgs a, RelPlan p)
             } else {
                 sum = lanes_sum<LANES>(sum);
             }
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-            for (int e = 0; e < 8 * NV; ++e) z[e] *= inv;
+            const float inv = sum == 0.0f ? 0.0f : recip_of<EXACT>(sum);
+            const __amdgpu_buffer_rsrc_t out = buffer_at(static_cast<T *>(a.out) + line * a.K);
+            const uint32_t off = on ? 0u : kNowhere;
+            const int tail = a.K & 7;
             if constexpr (!BACK) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     const int k0 = first + STEP * j;
-                    if (on && k0 < a.K) {
-                        if (a.drop.below) drop_values<8>(z + 8 * j, line * Kp + k0, a.drop);
-                        store_first(static_cast<T *>(a.out) + line * a.K + k0, z + 8 * j, a.K - k0);
+                    const uint32_t place = static_cast<uint32_t>(k0) * sizeof(T) | off;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+                    if (wave_first + STEP * j < end) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = z[8 * j + e] * inv;
+                        if (a.drop.below) drop_values<8>(v, line * Kp + k0, a.drop);
                     }
+                    store_row(out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail, v, T{});
                 }
             } else {
                 float dot = 0.0f, d[8];
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
-                    keep_bits(r.d[j], r.seen[j]);                      // whatever stands where nothing is seen
-                    if (a.drop.below) drop_raw(r.d[j], line * Kp + first + STEP * j, a.drop);
-                    r.d[j].widen(d);
+                    if (wave_first + STEP * j < end) {
+                        if (a.drop.below) drop_raw(r.d[j], static_cast<uint32_t>((line * Kp + first + STEP * j) >> 1), a.drop);
+                        r.d[j].widen(d);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(z[8 * j + e], d[e], dot);
+                        for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(z[8 * j + e], d[e], dot);
+                    }
                 }
                 if constexpr (WIDE) {
                     dot = lanes_sum<64>(dot);
                     if ((tid & 63) == 0) red[8 + (tid >> 6)] = dot;
                     __syncthreads();
-                    dot = keep * ((red[8] + red[9]) + (red[10] + red[11]));
+                    dot = (red[8] + red[9]) + (red[10] + red[11]);
                 } else {
-                    dot = keep * lanes_sum<LANES>(dot);
+                    dot = lanes_sum<LANES>(dot);
                 }
+                // z holds p / inv, d holds dp / keep, dot their product's sum:  dz = p (dp - sum p dp)
+                const float gain = keep * inv, minus = -(dot * inv) * gain;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     const int k0 = first + STEP * j;
-                    if (!on || k0 >= a.K) continue;
-                    r.d[j].widen(d);
-                    float dz[8];
+                    const uint32_t place = static_cast<uint32_t>(k0) * sizeof(T) | off;
+                    if (wave_first + STEP * j < end) {
+                        r.d[j].widen(d);
+                        float dz[8], was[8];
+                        places(j, q, [&](int e, int at) { was[e] = mine[at]; });
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dz[e] = z[8 * j + e] * __builtin_fmaf(d[e], keep, -dot);
-                        d[e] = dz[e] * a.scale;
+                        for (int e = 0; e < 8; ++e) {
+                            dz[e] = z[8 * j + e] * __builtin_fmaf(d[e], gain, minus);
+                            d[e] = dz[e] * a.scale;
+                        }
+                        if (k0 < a.K) {
+                            if constexpr (GRID) {
+                                places(j, q, [&](int e, int at) {
+                                    if (k0 + e < a.K) mine[at] = was[e] + dz[e];
+                                });
+                            } else {
+                                places(j, q, [&](int e, int at) { mine[at] = was[e] + dz[e]; });
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) d[e] = 0.0f;
                     }
-                    if (r.seen[j]) {
-                        float was[8];
-                        places(j, q, [&](int e, int at, bool) { was[e] = mine[at]; });
-                        places(j, q, [&](int e, int at, bool in) {
-                            if (in) mine[at] = was[e] + dz[e];
-                        });
-                    }
-                    store_first(static_cast<T *>(a.out) + line * a.K + k0, d, a.K - k0);
+                    store_row(out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail, d, T{});
                 }
             }
         }
     }
     if constexpr (BACK) {
         __syncthreads();
-        rel_write_sums(a, p, job, lds, [&](int i) {
+        rel_write_sums(a, p, job, lds, ids, [&](int i) {
             const int at = GRID ? i : padded(i);
             float t = sums[at];
 #pragma unroll
@@ -581,7 +816,7 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
     __shared__ float part[16][64];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = blockIdx.y;
     const int c0 = blockIdx.x * 64, c1 = min(a.n_buckets, c0 + 64);
-    const int gw = a.grid_w, rc = rel_const(a.Q, a.K, gw), parts = p.q_blocks * p.b_chunks, ulast = rel_u(a.K - 1, gw);
+    const int gw = a.grid_w, rc = rel_const(a.Q, a.K, gw), parts = p.q_blocks * p.b_chunks;
     const float *w = a.ws + static_cast<int64_t>(h) * parts * p.stride;
     float acc = 0.0f;                                     // of bucket c0 + lane, in wavefront 0
     for (int r0 = 0; r0 < n_rel; r0 += 1024) {
@@ -610,7 +845,7 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
                 for (int i = 0; i < 4; ++i) {
                     const int kk = k + 16 * i, qb = kk / p.b_chunks;
                     const int q0 = qb * p.q_block, q1 = min(a.Q, q0 + p.q_block), at = r - (rc - rel_u(q1 - 1, gw));
-                    const bool reach = kk < parts && r >= 0 && at >= 0 && at <= ulast - rel_u(q0, gw) + rel_u(q1 - 1, gw);
+                    const bool reach = kk < parts && r >= 0 && at >= 0 && r <= rel_last(a.Q, a.K, gw, a.causal, q0);
                     v[i] = reach ? w[static_cast<int64_t>(kk) * p.stride + at] : 0.0f;
                 }
 #pragma unroll
@@ -643,7 +878,10 @@ static hipError_t run(void (*f)(RelArgs, RelPlan), const RelArgs &a, const RelPl
     const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.H) * p.q_blocks * p.b_chunks);
     const size_t lds = rel_lds_bytes(p, a.grid_w, back);
     if (lds > 65536)
-        if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds))) return e;
+        if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds))) {
+            (void)hipGetLastError();
+            return e;
+        }
     f<<<blocks, kThreads, lds, st>>>(a, p);
     return hipGetLastError();
 }
@@ -656,12 +894,13 @@ static hipError_t by_length(const RelArgs &a, const RelPlan &p, hipStream_t st)
         case 8 * 16 + 1: return run(k_rel_rows<T, 8, BACK>, a, p, BACK, st);
         case 16 * 16 + 1: return run(k_rel_rows<T, 16, BACK>, a, p, BACK, st);
         case 32 * 16 + 1: return run(k_rel_rows<T, 32, BACK>, a, p, BACK, st);
-        case 64 * 16 + 1: return run(grid ? k_rel_long<T, 64, 1, true, BACK> : k_rel_long<T, 64, 1, false, BACK>, a, p, BACK, st);
-        case 64 * 16 + 2: return run(grid ? k_rel_long<T, 64, 2, true, BACK> : k_rel_long<T, 64, 2, false, BACK>, a, p, BACK, st);
-        case 64 * 16 + 4: return run(grid ? k_rel_long<T, 64, 4, true, BACK> : k_rel_long<T, 64, 4, false, BACK>, a, p, BACK, st);
-        case 256 * 16 + 2: return run(grid ? k_rel_long<T, 256, 2, true, BACK> : k_rel_long<T, 256, 2, false, BACK>, a, p, BACK, st);
-        case 256 * 16 + 4: return run(k_rel_long<T, 256, 4, false, BACK>, a, p, BACK, st);
-        default: return run(k_rel_long<T, 256, 8, false, BACK>, a, p, BACK, st);
+        case 64 * 16 + 1: return run(grid ? k_rel_long<T, 64, 1, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 64, 1, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
+        case 64 * 16 + 2: return run(grid ? k_rel_long<T, 64, 2, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 64, 2, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
+        case 64 * 16 + 4: return run(grid ? k_rel_long<T, 64, 4, true, BACK, LONG_AHEAD, LONG_WAVES> : k_rel_long<T, 64, 4, false, BACK, LONG_AHEAD, LONG_WAVES>, a, p, BACK, st);
+        case 256 * 16 + 1: return run(grid ? k_rel_long<T, 256, 1, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 256, 1, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
+        case 256 * 16 + 2: return run(grid ? k_rel_long<T, 256, 2, true, BACK, false, 1> : k_rel_long<T, 256, 2, false, BACK, false, 1>, a, p, BACK, st);
+        case 256 * 16 + 4: return run(k_rel_long<T, 256, 4, false, BACK, false, 1>, a, p, BACK, st);
+        default: return run(k_rel_long<T, 256, 8, false, BACK, false, 1>, a, p, BACK, st);
     }
 }
 
