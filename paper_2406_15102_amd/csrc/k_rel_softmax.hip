@@ -24,7 +24,28 @@
 #endif
 namespace hlq {
 
+// Where keys and queries lie: rel(q, k) = u(k) - u(q) + base.  Lines of a grid by a multiplication: exact for places below 2^16, of which a
+// grid has fewer, and no more lines than that.
+struct RelMap {
+    int w;                       // width of the grid (at least 2), 0: a sequence
+    uint32_t magic;              // 2^32 / w, rounded up
+    int base;
+    int ulast;                   // u of the last key
+    int seen;                    // with a causal map nothing is seen beyond this relative position
+    __host__ __device__ __forceinline__ int line(int k) const { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(k)) * magic) >> 32); }
+    __host__ __device__ __forceinline__ int u(int k) const { return w ? k + line(k) * (w - 1) : k; }
+    __host__ __device__ __forceinline__ int column(int k) const { return k - line(k) * w; }
+    // first and last relative position that queries q0 .. q1 - 1 reach
+    __host__ __device__ __forceinline__ int first(int q1) const { return base - u(q1 - 1); }
+    __host__ __device__ __forceinline__ int last(int q0) const
+    {
+        const int l = base + ulast - u(q0);
+        return seen < l ? seen : l;
+    }
+};
+
 struct RelPlan {
+    RelMap map;
     int lanes, nv;               // lanes of a row, vectors of 8 keys a lane
     int rows_q, rows_b;          // queries and batches that a workgroup's rows are in one step
     int q_block, q_blocks;       // queries of a workgroup
@@ -41,38 +62,34 @@ constexpr int kFewBuckets = 64;                                  // a lane of a 
 constexpr int kMaxKeysSequence = 16384, kMaxKeysGrid = 4096;     // two vectors of them (u stretches a grid's to two each) in LDS
 constexpr int kMaxKeysFew = 8192;                                // beside them, a byte for each
 
-__host__ __device__ __forceinline__ int rel_u(int k, int gw) { return gw ? k / gw * (2 * gw - 1) + k % gw : k; }
-// rel(q, k) = u(k) - u(q) + rel_const
-__host__ __device__ __forceinline__ int rel_const(int Q, int K, int gw) { return gw ? rel_u(K - 1, gw) : Q - 1; }
-
-// the last relative position that queries from q0 on reach; with a causal map they see none of those beyond rel_const, moved by K - Q
-__host__ __device__ __forceinline__ int rel_last(int Q, int K, int gw, int causal, int q0)
+RelMap rel_map(const RelArgs &a)
 {
-    const int rc = rel_const(Q, K, gw), last = rc + rel_u(K - 1, gw) - rel_u(q0, gw), seen = rc + (gw ? 0 : K - Q);
-    return causal && seen < last ? seen : last;
+    RelMap m{};
+    m.w = a.grid_w > 1 ? a.grid_w : 0;            // a grid of one column is a sequence
+    m.magic = m.w ? static_cast<uint32_t>(((uint64_t(1) << 32) + m.w - 1) / m.w) : 0;
+    m.ulast = m.u(a.K - 1);
+    m.base = m.w ? m.ulast : a.Q - 1;
+    m.seen = a.causal ? m.base + (m.w ? 0 : a.K - a.Q) : INT32_MAX;
+    return m;
 }
 
 // Place of relative position i of a sequence in LDS: one float of padding to eight, so that lanes that read element e of their eight keys,
 // 8 floats apart, meet 64 banks instead of 8.
 __host__ __device__ __forceinline__ int padded(int i) { return i + (i >> 3); }
 
-// Workgroups that the steps are dealt to, at most: those that are resident at once (256 compute units), twice where queries differ in their work.
-int64_t rel_blocks(const RelPlan &p, bool back, bool uneven)
-{
-#ifndef RB_ROWS
-#define RB_ROWS 5
-#define RB_LONG 3
-#define RB_WIDE 6
-#define RB_FWD 7
-#define RB_UNEVEN 2
+// workgroups that a compute unit holds at once, by registers and LDS
+int rel_resident(const RelPlan &p, bool back) { return back ? (p.lanes < 64 ? 5 : p.lanes < 256 ? 3 : 6) : 7; }
+#ifndef KSETUP
+#define KSETUP 5
+#define KCOVER 3
 #endif
-    const int resident = back ? (p.lanes < 64 ? RB_ROWS : p.lanes < 256 ? RB_LONG : RB_WIDE) : RB_FWD;
-    return static_cast<int64_t>(256) * resident * (uneven && p.lanes >= 64 ? RB_UNEVEN : 1);
-}
+constexpr int64_t kSetup = KSETUP, kCover = KCOVER;
 
 RelPlan rel_plan(const RelArgs &a, bool back)
 {
     RelPlan p{};
+    p.map = rel_map(a);
+    const int gw = p.map.w;
     if (a.K <= 64) p.lanes = 8, p.nv = 1;
     else if (a.K <= 128) p.lanes = 16, p.nv = 1;
     else if (a.K <= 256) p.lanes = 32, p.nv = 1;
@@ -89,15 +106,22 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     // what a row of another batch is away fits 32 bits (bytes of fp32)
     while (p.rows_b > 1 && (p.rows_b - 1) * (static_cast<int64_t>(a.H) * a.Q * a.K) >= int64_t(1) << 28) p.rows_b /= 2, p.rows_q *= 2;
     const int q_steps = (a.Q + p.rows_q - 1) / p.rows_q, b_steps = (a.B + p.rows_b - 1) / p.rows_b;
-    // Steps to a workgroup: all batches of a query first (its bias and their sum stay in registers, or the vector in LDS serves more rows), then more
-    // queries, until the workgroups are no more than `most_blocks`; then as even as they come.
-    const int64_t most_blocks = rel_blocks(p, back, a.causal != 0);
-    const int64_t steps = static_cast<int64_t>(a.H) * q_steps * b_steps;
-    int b_per = static_cast<int>(std::min<int64_t>(b_steps, std::max<int64_t>(1, steps / most_blocks)));
-    while (b_per < b_steps && static_cast<int64_t>(a.H) * q_steps * ((b_steps + b_per - 1) / b_per) > most_blocks) ++b_per;
-    const int chunks = (b_steps + b_per - 1) / b_per;
-    b_per = (b_steps + chunks - 1) / chunks;
-    int q_per = static_cast<int>(std::min<int64_t>(q_steps, std::max<int64_t>(1, (static_cast<int64_t>(a.H) * q_steps * chunks + most_blocks - 1) / most_blocks)));
+    // A step is one row of each group of lanes.  A workgroup goes through the batch with one query's bias in registers, then on to more queries
+    // with the vectors that it has in LDS; what it costs before and after comes to kSetup steps.  The chip's 256 compute units take
+    // the workgroups in equal shares, so what counts is the largest share; with fewer than kCover of them at once a unit waits for memory.
+    const int64_t lines = static_cast<int64_t>(a.H) * q_steps;                 // workgroups, were each to take one step's queries and all batches
+    const int resident = rel_resident(p, back);
+    int chunks = 1, q_per = 1;
+    int64_t best = INT64_MAX;
+    for (int m = 1; m <= resident; ++m) {
+        const int64_t target = 256 * m;
+        const int n = static_cast<int>(std::min<int64_t>(b_steps, std::max<int64_t>(1, target / lines)));
+        const int per = static_cast<int>(std::min<int64_t>(q_steps, std::max<int64_t>(1, (lines + target - 1) / target)));
+        const int64_t share = (static_cast<int64_t>(a.H) * ((q_steps + per - 1) / per) * n + 255) / 256;
+        const int64_t cost = std::max(kCover, share) * (static_cast<int64_t>(per) * ((b_steps + n - 1) / n) + kSetup);
+        if (cost < best) best = cost, chunks = n, q_per = per;
+    }
+    int b_per = (b_steps + chunks - 1) / chunks;
     if (q_per * p.rows_q > 512) q_per = 512 / p.rows_q;         // the reach of a workgroup's queries stays in LDS
     const int blocks = (q_steps + q_per - 1) / q_per;
     q_per = (q_steps + blocks - 1) / blocks;
@@ -106,10 +130,9 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     p.b_chunk = b_per * p.rows_b;
     p.b_chunks = (a.B + p.b_chunk - 1) / p.b_chunk;
     // reach of q_block consecutive queries
-    const int most = a.grid_w ? (p.q_block + a.grid_w - 1) / a.grid_w * (2 * a.grid_w - 1) + a.grid_w : p.q_block;
-    const int all = a.grid_w ? 2 * rel_u(a.K - 1, a.grid_w) + 1 : a.Q + a.K - 1;
-    p.win = rel_u(a.K - 1, a.grid_w) + most;
-    if (p.win > all) p.win = all;
+    const int most = gw ? (p.q_block + gw - 1) / gw * (2 * gw - 1) + gw : p.q_block;
+    const int all = gw ? 2 * p.map.ulast + 1 : a.Q + a.K - 1;
+    p.win = std::min(p.map.ulast + most, all);
     p.few = a.n_buckets <= kFewBuckets && a.K <= kMaxKeysFew;
     p.stride = p.few ? kFewBuckets : p.win;
     return p;
@@ -118,13 +141,13 @@ RelPlan rel_plan(const RelArgs &a, bool back)
 // LDS of a workgroup, in floats: the bias vector, the sums by relative position (one vector a wavefront where a wavefront is a row; for
 // shorter rows one, and the rows' sums over the batch), reductions across the wavefronts.
 // A sequence's vectors have room for every place that a row's lanes may reach, keys or not.
-__host__ __device__ __forceinline__ int rel_vector(const RelPlan &p, int gw)
+__host__ __device__ __forceinline__ int rel_vector(const RelPlan &p)
 {
-    return p.lanes >= 64 && !gw ? padded(p.lanes * p.nv * 8 + p.q_block) : p.win;
+    return p.lanes >= 64 && !p.map.w ? padded(p.lanes * p.nv * 8 + p.q_block) : p.win;
 }
-size_t rel_lds_bytes(const RelPlan &p, int gw, bool back)
+size_t rel_lds_bytes(const RelPlan &p, bool back)
 {
-    const size_t v = rel_vector(p, gw);
+    const size_t v = rel_vector(p);
     const int rows = kThreads / p.lanes;
     size_t n = v + 16 + (back && p.few ? (p.win + 3) / 4 : 0);
     if (back) n += p.lanes == 64 ? 4 * v : v + (rows > 1 ? static_cast<size_t>(rows) * p.lanes * p.nv * 8 : 0);
@@ -276,7 +299,8 @@ template <bool EXACT> struct RowExp {
 
 // What a workgroup works on, the same for all its threads.
 struct RelJob {
-    int h, q0, q1, b0, b1, part, rc, rlo, win;
+    int h, q0, q1, b0, b1, part;
+    int rlo, win;                // first relative position that its queries reach, and how many
 };
 __device__ __forceinline__ RelJob rel_job(const RelArgs &a, const RelPlan &p)
 {
@@ -294,36 +318,55 @@ __device__ __forceinline__ RelJob rel_job(const RelArgs &a, const RelPlan &p)
     j.q0 = qb * p.q_block, j.q1 = min(a.Q, j.q0 + p.q_block);
     j.b0 = bc * p.b_chunk, j.b1 = min(a.B, j.b0 + p.b_chunk);
     j.part = qb * p.b_chunks + bc;
-    j.rc = rel_const(a.Q, a.K, a.grid_w);
-    j.rlo = j.rc - rel_u(j.q1 - 1, a.grid_w);                         // the first relative position that its queries reach
-    j.win = rel_last(a.Q, a.K, a.grid_w, a.causal, j.q0) - j.rlo + 1;
+    j.rlo = p.map.first(j.q1);
+    j.win = p.map.last(j.q0) - j.rlo + 1;
     return j;
 }
 
-// The head's bias of the workgroup's relative positions to bias[place(i)], their buckets to ids[i] where they are few.  The loads of four go out
-// before the first is used: one after the other their latency, twice, is most of a short workgroup's time.
+// The head's bias of the workgroup's relative positions to bias[place(i)], their buckets to ids[i] where they are few.  A short workgroup spends
+// most of its time on the latency of these loads: those of eight positions go out before the first is used, and up to 64 buckets of the
+// head are fetched beside them, not behind them.
 template <typename Place>
 __device__ __forceinline__ void rel_fill(const RelArgs &a, const RelPlan &p, const RelJob &job, float *bias, uint8_t *ids, Place place)
 {
-    for (int i0 = threadIdx.x; i0 < job.win; i0 += 4 * kThreads) {
-        int c[4];
-        float t[4];
+    constexpr int AT_ONCE = 8;
+    __shared__ float column[kFewBuckets];
+    const bool small = a.n_buckets <= kFewBuckets;
+    int c[AT_ONCE];
+    auto fetch = [&](int first) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) c[u] = i0 + u * kThreads < job.win ? a.of[job.rlo + i0 + u * kThreads] : -1;
+        for (int u = 0; u < AT_ONCE; ++u) {
+            c[u] = -1;
+            if (first + u * kThreads < job.win) {            // the same for the workgroup
+                const int i = first + u * kThreads + threadIdx.x;
+                if (i < job.win) c[u] = a.of[job.rlo + i];
+            }
+        }
+    };
+    fetch(0);
+    if (small) {
+        if (static_cast<int>(threadIdx.x) < a.n_buckets) column[threadIdx.x] = load_param(a.table, a.param_f32, static_cast<int64_t>(threadIdx.x) * a.H + job.h);
+        __syncthreads();
+    }
+    for (int first = 0; first < job.win; first += AT_ONCE * kThreads) {
+        float t[AT_ONCE];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (first + u * kThreads >= job.win) continue;
             const bool has = c[u] >= 0 && c[u] < a.n_buckets;
-            t[u] = has ? load_param(a.table, a.param_f32, static_cast<int64_t>(c[u]) * a.H + job.h) : 0.0f;
+            t[u] = 0.0f;
+            if (has) t[u] = small ? column[c[u]] : load_param(a.table, a.param_f32, static_cast<int64_t>(c[u]) * a.H + job.h);
             c[u] = has ? c[u] : 255;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * kThreads;
-            if (i < job.win) {
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int i = first + u * kThreads + threadIdx.x;
+            if (first + u * kThreads < job.win && i < job.win) {
                 bias[place(i)] = t[u];
                 if (ids && p.few) ids[i] = static_cast<uint8_t>(c[u]);
             }
         }
+        fetch(first + AT_ONCE * kThreads);
     }
 }
 
@@ -369,13 +412,25 @@ template <typename T, int NV, bool BACK> struct RelRow {
     }
 };
 
-// the bucket's lane adds v: lanes hold (bucket, or none of 0 .. 63, and value), acc of lane l is the sum of bucket l; whole wavefronts only
-__device__ __forceinline__ void bucket_add(int c, float v, float &acc)
+// The bucket's lane adds v: lanes hold (bucket, or none of 0 .. 63, and value), acc of lane l is the sum of bucket l; whole wavefronts only.
+// `owner`: 64 words of LDS of the wavefront's own.  Far distances share a bucket; where no two lanes do, a bucket's lane fetches
+// the value; else one lane after the other.
+__device__ __forceinline__ void bucket_add(int c, float v, float &acc, int *owner)
 {
     const int lane = threadIdx.x & 63, c0 = __builtin_amdgcn_readfirstlane(c);
-    if (__all(c == c0)) {                            // far distances share a bucket
+    if (__all(c == c0)) {
         v = lanes_sum<64>(v);
         acc += lane == c0 ? v : 0.0f;
+        return;
+    }
+    const bool in = c >= 0 && c < 64;
+    volatile int *own = owner;
+    own[lane] = -1;
+    if (in) own[c] = lane;
+    if (__all(!in || own[c] == lane)) {
+        const int from = own[lane];
+        const float x = __shfl(v, from & 63);
+        acc += from >= 0 ? x : 0.0f;
     } else {
         for (int i = 0; i < 64; ++i) {
             const int ci = __builtin_amdgcn_readlane(c, i);
@@ -389,6 +444,7 @@ __device__ __forceinline__ void bucket_add(int c, float v, float &acc)
 template <typename Value>
 __device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &p, const RelJob &job, float *lds, const uint8_t *ids, Value value)
 {
+    __shared__ int owner[kThreads / 64][64];
     const int tid = threadIdx.x;
     float *w = a.ws + (static_cast<int64_t>(job.h) * p.q_blocks * p.b_chunks + job.part) * p.stride;
     if (!p.few) {
@@ -398,7 +454,7 @@ __device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &
     float acc = 0.0f;
     for (int i0 = tid & ~63; i0 < job.win; i0 += kThreads) {
         const int i = i0 + (tid & 63);
-        bucket_add(i < job.win ? ids[i] : 255, i < job.win ? value(i) : 0.0f, acc);
+        bucket_add(i < job.win ? ids[i] : 255, i < job.win ? value(i) : 0.0f, acc, owner[tid >> 6]);
     }
     __syncthreads();
     lds[tid] = acc;
@@ -451,7 +507,7 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
     const float NONE = -__builtin_inff();
     const int tid = threadIdx.x, row = tid / LANES, lane = tid % LANES, k0 = lane * 8;
     const RelJob job = rel_job(a, p);
-    const int gw = a.grid_w;
+    const int gw = p.map.w;
     float *bias = lds, *accw = bias + p.win, *tile = accw + (BACK ? p.win : 0);
     uint8_t *ids = BACK ? reinterpret_cast<uint8_t *>(tile + ROWS * WIDTH) : nullptr;
     const int64_t plane = static_cast<int64_t>(a.H) * a.Q * a.K, total = a.B * plane, mask_total = static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K;
@@ -497,7 +553,7 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
         const bool whole = __all(bits == 0xFFu);
         float bv[8], acc[8];
         {
-            int i = rel_u(k0, gw) - rel_u(q < job.q1 ? q : job.q1 - 1, gw) + job.rc - job.rlo, kx = gw ? k0 % gw : 0;
+            int i = p.map.u(k0) + p.map.base - p.map.u(q < job.q1 ? q : job.q1 - 1) - job.rlo, kx = gw ? p.map.column(k0) : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 bv[e] = (bits >> e) & 1u ? bias[i] : NONE;
@@ -567,18 +623,23 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
             for (int e = 0; e < 8; ++e) tile[row * WIDTH + k0 + e] = acc[e];
             __syncthreads();
             const int qe = min(job.q1, qs + p.rows_q);
-            const int i0 = job.rc - rel_u(qe - 1, gw) - job.rlo, i1 = min(job.rc + rel_u(a.K - 1, gw) - rel_u(qs, gw) - job.rlo, job.win - 1);
+            const int i0 = p.map.first(qe) - job.rlo, i1 = p.map.last(qs) - job.rlo;
             for (int i = i0 + tid; i <= i1; i += kThreads) {
+                // queries lo <= q < hi meet this relative position at key q + step, on a grid for each line of the step's queries
                 float t = 0.0f;
-                const int rel = job.rlo + i - job.rc;                  // u(k) - u(q)
-                for (int y = 0; y < qe - qs; ++y) {
-                    int k = rel + qs + y;
-                    if (gw) {
-                        const int uk = rel + rel_u(qs + y, gw), ky = uk >= 0 ? uk / (2 * gw - 1) : -1, kx = uk - ky * (2 * gw - 1);
-                        k = uk >= 0 && kx < gw ? ky * gw + kx : -1;
-                    }
-                    if (k >= 0 && k < a.K)
-                        for (int x = 0; x < p.rows_b; ++x) t += tile[(x * p.rows_q + y) * WIDTH + k];
+                auto line = [&](int lo, int hi, int step) {
+                    const float *at = tile + (lo - qs) * WIDTH + lo + step;
+                    for (int q2 = lo; q2 < hi; ++q2, at += WIDTH + 1)
+                        for (int x = 0; x < p.rows_b; ++x) t += at[x * p.rows_q * WIDTH];
+                };
+                if (!gw) {
+                    const int step = job.rlo + i - p.map.base;
+                    line(max(qs, -step), min(qe, a.K - step), step);
+                } else {
+                    const int h = p.map.line(a.K), y = (job.rlo + i) / (2 * gw - 1), dx = job.rlo + i - y * (2 * gw - 1) - (gw - 1), dy = y - (h - 1);
+                    for (int qy = p.map.line(qs); qy * gw < qe; ++qy)
+                        if (qy + dy >= 0 && qy + dy < h)
+                            line(max(qs, qy * gw + max(0, -dx)), min(qe, qy * gw + min(gw, gw - dx)), dy * gw + dx);
                 }
                 accw[i] += t;
             }
@@ -601,8 +662,8 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
     const float NONE = -__builtin_inff();
     const int tid = threadIdx.x, row = tid / LANES, first = tid % LANES * 8;
     const RelJob job = rel_job(a, p);
-    const int gw = GRID ? a.grid_w : 0;
-    const int size = rel_vector(p, gw);
+    const int gw = GRID ? p.map.w : 0;
+    const int size = rel_vector(p);
     float *bias = lds, *sums = lds + size, *red = sums + VECTORS * size;
     uint8_t *ids = BACK ? reinterpret_cast<uint8_t *>(red + 16) : nullptr;
     const int64_t total = static_cast<int64_t>(a.B) * a.H * a.Q * a.K;
@@ -619,7 +680,7 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
     auto places = [&](int j, int q, auto f) {
         if constexpr (GRID) {
             const int k0 = min(first + STEP * j, (a.K - 1) & ~7);
-            int i = rel_u(k0, gw) - rel_u(q, gw) + job.rc - job.rlo, kx = k0 % gw;
+            int i = p.map.u(k0) + p.map.base - p.map.u(q) - job.rlo, kx = p.map.column(k0);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 f(e, min(i, size - 1));
@@ -628,7 +689,7 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
             }
         } else {
             // padded(k0 + shift + e), k0 a multiple of 8 and shift the wavefront's own: 9 k0 / 8 + padded(shift + e)
-            const int shift = job.rc - job.rlo - q, at = first + (first >> 3);
+            const int shift = p.map.base - job.rlo - q, at = first + (first >> 3);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f(e, at + padded(shift + e) + padded(STEP) * j);
         }
@@ -812,12 +873,13 @@ __global__ __launch_bounds__(1024) void k_rel_few_buckets(RelArgs a, RelPlan p)
 // to every 16th vector, and then to their buckets, a lane each.
 __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel)
 {
-    __shared__ int list[1024], of[1024], count[16];
+    __shared__ int list[1024], of[1024], count[16], owner[64];
     __shared__ float part[16][64];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, h = blockIdx.y;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = blockIdx.y;
     const int c0 = blockIdx.x * 64, c1 = min(a.n_buckets, c0 + 64);
-    const int gw = a.grid_w, rc = rel_const(a.Q, a.K, gw), parts = p.q_blocks * p.b_chunks;
+    const int parts = p.q_blocks * p.b_chunks;
     const float *w = a.ws + static_cast<int64_t>(h) * parts * p.stride;
+    const int step_q = p.b_chunks ? 16 / p.b_chunks : 0, step_b = p.b_chunks ? 16 % p.b_chunks : 0;
     float acc = 0.0f;                                     // of bucket c0 + lane, in wavefront 0
     for (int r0 = 0; r0 < n_rel; r0 += 1024) {
         const int c = r0 + tid < n_rel ? a.of[r0 + tid] : -1;
@@ -839,24 +901,27 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
         for (int e0 = 0; e0 < all; e0 += 64) {
             const int r = e0 + lane < all ? list[e0 + lane] : -1;
             float t = 0.0f;
-            for (int k = wave; k < parts; k += 16 * 4) {
-                float v[4];
+            int qb = wave / p.b_chunks, bc = wave - qb * p.b_chunks;              // the same for the wavefront, as what follows from them
+            for (int k = wave; k < parts; k += 16 * 12) {
+                float v[12];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int kk = k + 16 * i, qb = kk / p.b_chunks;
-                    const int q0 = qb * p.q_block, q1 = min(a.Q, q0 + p.q_block), at = r - (rc - rel_u(q1 - 1, gw));
-                    const bool reach = kk < parts && r >= 0 && at >= 0 && r <= rel_last(a.Q, a.K, gw, a.causal, q0);
-                    v[i] = reach ? w[static_cast<int64_t>(kk) * p.stride + at] : 0.0f;
+                for (int i = 0; i < 12; ++i) {
+                    const int q0 = qb * p.q_block, q1 = min(a.Q, q0 + p.q_block);
+                    const int lo = p.map.first(q1), hi = p.map.last(q0);
+                    v[i] = 0.0f;
+                    if (k + 16 * i < parts && r >= lo && r <= hi) v[i] = w[static_cast<int64_t>(k + 16 * i) * p.stride + r - lo];
+                    qb += step_q, bc += step_b;
+                    if (bc >= p.b_chunks) bc -= p.b_chunks, ++qb;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t += v[i];
+                for (int i = 0; i < 12; ++i) t += v[i];
             }
             part[wave][lane] = t;
             __syncthreads();
             if (wave == 0) {
                 t = part[0][lane];
                 for (int i = 1; i < 16; ++i) t += part[i][lane];
-                bucket_add(r >= 0 ? of[e0 + lane] : -1, t, acc);
+                bucket_add(r >= 0 ? of[e0 + lane] : -1, t, acc, owner);
             }
             __syncthreads();
         }
@@ -876,7 +941,7 @@ size_t rel_softmax_ws_bytes(const RelArgs &a)
 static hipError_t run(void (*f)(RelArgs, RelPlan), const RelArgs &a, const RelPlan &p, bool back, hipStream_t st)
 {
     const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.H) * p.q_blocks * p.b_chunks);
-    const size_t lds = rel_lds_bytes(p, a.grid_w, back);
+    const size_t lds = rel_lds_bytes(p, back);
     if (lds > 65536)
         if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds))) {
             (void)hipGetLastError();
@@ -889,7 +954,7 @@ static hipError_t run(void (*f)(RelArgs, RelPlan), const RelArgs &a, const RelPl
 template <typename T, bool BACK>
 static hipError_t by_length(const RelArgs &a, const RelPlan &p, hipStream_t st)
 {
-    const bool grid = a.grid_w != 0;
+    const bool grid = p.map.w != 0;
     switch (p.lanes * 16 + p.nv) {
         case 8 * 16 + 1: return run(k_rel_rows<T, 8, BACK>, a, p, BACK, st);
         case 16 * 16 + 1: return run(k_rel_rows<T, 16, BACK>, a, p, BACK, st);
@@ -916,7 +981,7 @@ hipError_t launch_rel_softmax_backward(const RelArgs &a, hipStream_t st)
     int n_rel = 0;
     if (a.B && a.Q && a.K) {
         p = rel_plan(a, true);
-        n_rel = a.grid_w ? 2 * rel_u(a.K - 1, a.grid_w) + 1 : a.Q + a.K - 1;
+        n_rel = p.map.w ? 2 * p.map.ulast + 1 : a.Q + a.K - 1;
         if (const hipError_t e = a.is_f32 ? by_length<float, true>(a, p, st) : by_length<bf16_t, true>(a, p, st)) return e;
     }
     if (!a.dtable) return hipSuccess;
