@@ -545,7 +545,7 @@ int hlq_dropout(const void *X, const void *residual, int64_t n, double p, uint64
  *   mean, rstd    [Nb, groups] fp32, for the backward call, or NULL
  *   workspace     >= hlq_group_norm_workspace_bytes(..., 0) bytes, 256-byte aligned (it may be 0: then none is used), or NULL for the
  *                 registered or library-owned one.
- * HLQ_ERR_SHAPE: P < 1, C % groups, an unknown act, eps not positive, Nb C >= 2^31, C > 2^24, or C / groups too large: up to 1024 is
+ * HLQ_ERR_SHAPE: P < 1, C % groups, an unknown act, eps not positive, Nb C >= 2^31, P > 2^30, C > 2^17, or C / groups too large: up to 1024 is
  * taken always, and up to 2048 where it is a multiple of 8.
  */
 #define HLQ_ACT_NONE 0

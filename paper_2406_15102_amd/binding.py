@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -496,104 +497,111 @@ def hlq_backward_products(Gq, sG, WqT, sW, gx_bits, GhatT, sGhat, XhatT, sXhat, 
 
 
 # ---- the operators around the products ----
+# Small calls are as long as what the host does for them: these functions look at each property of a tensor once.
+
+_BF16, _FP32 = torch.bfloat16, torch.float32
+_geom_fields = struct.Struct("9i").unpack_from
+
 
 def _dtype_code(dtype):
-    if dtype == torch.bfloat16:
+    if dtype is _BF16:
         return HLQ_BF16
-    if dtype == torch.float32:
+    if dtype is _FP32:
         return HLQ_F32
     raise TypeError("element type must be bfloat16 or float32, got %s" % dtype)
 
 
-def _expect_like(name, t, like):
-    if t is not None and (t.dtype != like.dtype or t.shape != like.shape):
-        raise ValueError("%s must be %s %s like the input, got %s %s" % (name, like.dtype, tuple(like.shape), t.dtype, tuple(t.shape)))
-
-
-def _expect_vector(name, t, shape, dtype):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
-        raise ValueError("%s must be %s %s, got %s %s" % (name, dtype, shape, t.dtype, tuple(t.shape)))
+def _dense(name, t, n, dtype):
+    """Address of a dense GPU tensor of n elements of that type, None for None: as with _expect, what the C call reads and writes."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n:
+        raise ValueError("%s must hold %d elements of %s, has %s of %s" % (name, n, dtype, tuple(t.shape), t.dtype))
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous (dense row-major)")
+    if not t.is_cuda:
+        raise ValueError("tensor must live on the GPU")
+    return t.data_ptr()
 
 
 def hlq_dropout(X, residual, p, seed, Y):
     """Y <- residual + dropout(X) (residual None: dropout(X)); the backward pass is the same call on the gradient."""
-    _expect_like("residual", residual, X)
-    _expect_like("Y", Y, X)
-    _check(lib().hlq_dropout(_ptr(X), _ptr(residual), X.numel(), p, seed, _dt(X), _ptr(Y), _stream()), "hlq_dropout")
+    n, dt = X.numel(), X.dtype
+    _check((_lib or lib()).hlq_dropout(_dense("X", X, n, dt), _dense("residual", residual, n, dt), n, p, seed, _dtype_code(dt),
+                                       _dense("Y", Y, n, dt), _stream()), "hlq_dropout")
 
 
 def hlq_group_norm_workspace_bytes(Nb, P, C_, groups, dtype, backward=False) -> int:
     return int(lib().hlq_group_norm_workspace_bytes(Nb, P, C_, groups, _dtype_code(dtype), int(bool(backward))))
 
 
-def _group_norm_sizes(X, weight, bias, groups):
-    """(Nb, P, C, element type of the parameters) of channels-last X [Nb, ..., C]"""
-    if X.dim() < 2:
-        raise ValueError("X must be [Nb, ..., C], got %s" % (tuple(X.shape),))
-    Nb, C_ = X.shape[0], X.shape[-1]
+def _group_norm_sizes(X):
+    """(elements, Nb, P, C) of channels-last X [Nb, ..., C]"""
+    shape, n = X.shape, X.numel()
+    if len(shape) < 2:
+        raise ValueError("X must be [Nb, ..., C], got %s" % (tuple(shape),))
+    Nb, C_ = shape[0], shape[-1]
+    if n:
+        return n, Nb, n // (Nb * C_), C_
     P = 1
-    for d in X.shape[1:-1]:
+    for d in shape[1:-1]:
         P *= d
-    params = weight if weight is not None else bias
-    pdt = torch.float32 if params is None else params.dtype
-    _expect_vector("weight", weight, (C_,), pdt)
-    _expect_vector("bias", bias, (C_,), pdt)
-    return Nb, P, C_, pdt
+    return n, Nb, P, C_
 
 
 def hlq_group_norm_act(X, weight, bias, groups, eps, act, Y, mean=None, rstd=None, workspace=None, p=0.0, seed=0):
     """Y <- dropout(act(GroupNorm(X) weight + bias)) of channels-last X [Nb, ..., C]; mean, rstd [Nb, groups] fp32 for the backward call."""
-    Nb, P, C_, pdt = _group_norm_sizes(X, weight, bias, groups)
-    _expect_like("Y", Y, X)
-    _expect_vector("mean", mean, (Nb, groups), torch.float32)
-    _expect_vector("rstd", rstd, (Nb, groups), torch.float32)
+    n, Nb, P, C_ = _group_norm_sizes(X)
+    dt, stats = X.dtype, Nb * groups
+    pdt = weight.dtype if weight is not None else (_FP32 if bias is None else bias.dtype)
     wp, wb = _ws(workspace)
-    _check(lib().hlq_group_norm_act(_ptr(X), _ptr(weight), _ptr(bias), Nb, P, C_, groups, eps, act, p, seed, _dt(X), _dtype_code(pdt),
-                                    _ptr(Y), _ptr(mean), _ptr(rstd), wp, wb, _stream()), "hlq_group_norm_act")
+    _check((_lib or lib()).hlq_group_norm_act(
+        _dense("X", X, n, dt), _dense("weight", weight, C_, pdt), _dense("bias", bias, C_, pdt), Nb, P, C_, groups, eps, act, p, seed,
+        _dtype_code(dt), _dtype_code(pdt), _dense("Y", Y, n, dt), _dense("mean", mean, stats, _FP32), _dense("rstd", rstd, stats, _FP32),
+        wp, wb, _stream()), "hlq_group_norm_act")
 
 
 def hlq_group_norm_act_backward(dY, X, weight, bias, mean, rstd, groups, act, dX, dweight, dbias, workspace=None, p=0.0, seed=0):
     """dX, dweight, dbias <- gradients of hlq_group_norm_act with the same arguments; any of the three may be None."""
-    Nb, P, C_, pdt = _group_norm_sizes(X, weight, bias, groups)
-    if weight is None and bias is None:
-        pdt = dweight.dtype if dweight is not None else (dbias.dtype if dbias is not None else pdt)
-    _expect_like("dY", dY, X)
-    _expect_like("dX", dX, X)
-    _expect_vector("mean", mean, (Nb, groups), torch.float32)
-    _expect_vector("rstd", rstd, (Nb, groups), torch.float32)
-    _expect_vector("dweight", dweight, (C_,), pdt)
-    _expect_vector("dbias", dbias, (C_,), pdt)
+    n, Nb, P, C_ = _group_norm_sizes(X)
+    dt, stats, pdt = X.dtype, Nb * groups, _FP32
+    for t in (weight, bias, dweight, dbias):
+        if t is not None:
+            pdt = t.dtype
+            break
     wp, wb = _ws(workspace)
-    _check(lib().hlq_group_norm_act_backward(_ptr(dY), _ptr(X), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), Nb, P, C_, groups, act,
-                                             p, seed, _dt(X), _dtype_code(pdt), _ptr(dX), _ptr(dweight), _ptr(dbias), wp, wb, _stream()),
-           "hlq_group_norm_act_backward")
+    _check((_lib or lib()).hlq_group_norm_act_backward(
+        _dense("dY", dY, n, dt), _dense("X", X, n, dt), _dense("weight", weight, C_, pdt), _dense("bias", bias, C_, pdt),
+        _dense("mean", mean, stats, _FP32), _dense("rstd", rstd, stats, _FP32), Nb, P, C_, groups, act, p, seed,
+        _dtype_code(dt), _dtype_code(pdt), _dense("dX", dX, n, dt), _dense("dweight", dweight, C_, pdt), _dense("dbias", dbias, C_, pdt),
+        wp, wb, _stream()), "hlq_group_norm_act_backward")
+
+
+def _rel_positions(Q, K, w):
+    return (2 * (K // w) - 1) * (2 * w - 1) if w else max(0, Q + K - 1)
 
 
 def hlq_rel_positions(geom) -> int:
     """Number of relative positions of a map: the length of `buckets`."""
-    if geom.grid_w:
-        return (2 * (geom.K // geom.grid_w) - 1) * (2 * geom.grid_w - 1)
-    return max(0, geom.Q + geom.K - 1)
+    return _rel_positions(geom.Q, geom.K, geom.grid_w)
 
 
-def _expect_rel(S, table, buckets, mask, geom):
-    if tuple(S.shape) != (geom.B, geom.H, geom.Q, geom.K):
-        raise ValueError("scores must be %s, got %s" % ((geom.B, geom.H, geom.Q, geom.K), tuple(S.shape)))
-    _expect_vector("table", table, (geom.n_buckets, geom.H), table.dtype)
-    _expect_vector("buckets", buckets, (hlq_rel_positions(geom),), torch.int32)
-    if (mask is None) != (geom.mask_batches == 0):
+def _rel_tensors(S, table, buckets, mask, geom):
+    """(elements of a map, of the table, addresses of S, table, buckets and mask), checked against the geometry"""
+    B, H, Q, K, w, n_buckets, _, mask_batches, mask_rows = _geom_fields(geom)
+    if (mask is None) != (mask_batches == 0):
         raise ValueError("mask and geom.mask_batches do not agree")
-    if mask is not None:
-        if mask.dtype not in (torch.uint8, torch.bool) or tuple(mask.shape) != (geom.mask_batches, geom.mask_rows, geom.K):
-            raise ValueError("mask must be bytes %s, got %s %s" % ((geom.mask_batches, geom.mask_rows, geom.K), mask.dtype, tuple(mask.shape)))
+    n, nt = B * H * Q * K, n_buckets * H
+    return (n, nt, _dense("scores", S, n, S.dtype), _dense("table", table, nt, table.dtype), _dense("buckets", buckets, _rel_positions(Q, K, w), torch.int32),
+            None if mask is None else _dense("mask", mask, mask_batches * mask_rows * K, torch.bool if mask.dtype is torch.bool else torch.uint8))
 
 
 def hlq_rel_softmax(S, table, buckets, mask, geom, scale, P, p=0.0, seed=0):
     """P <- dropout(softmax(scale S + bias)), the bias of a key by its position relative to the query."""
-    _expect_rel(S, table, buckets, mask, geom)
-    _expect_like("P", P, S)
-    _check(lib().hlq_rel_softmax(_ptr(S), _ptr(table), _ptr(buckets), _ptr(mask), C.byref(geom), scale, p, seed, _dt(S), _dt(table),
-                                 _ptr(P), _stream()), "hlq_rel_softmax")
+    n, _, s, t, b, m = _rel_tensors(S, table, buckets, mask, geom)
+    dt = S.dtype
+    _check((_lib or lib()).hlq_rel_softmax(s, t, b, m, C.byref(geom), scale, p, seed, _dtype_code(dt), _dtype_code(table.dtype),
+                                           _dense("P", P, n, dt), _stream()), "hlq_rel_softmax")
 
 
 def hlq_rel_softmax_workspace_bytes(geom, dtype) -> int:
@@ -602,10 +610,9 @@ def hlq_rel_softmax_workspace_bytes(geom, dtype) -> int:
 
 def hlq_rel_softmax_backward(dP, S, table, buckets, mask, geom, scale, dS, dtable=None, workspace=None, p=0.0, seed=0):
     """dS, dtable <- gradients of hlq_rel_softmax with the same arguments; dtable may be None."""
-    _expect_rel(S, table, buckets, mask, geom)
-    _expect_like("dP", dP, S)
-    _expect_like("dS", dS, S)
-    _expect_vector("dtable", dtable, tuple(table.shape), table.dtype)
+    n, nt, s, t, b, m = _rel_tensors(S, table, buckets, mask, geom)
+    dt, tdt = S.dtype, table.dtype
     wp, wb = _ws(workspace)
-    _check(lib().hlq_rel_softmax_backward(_ptr(dP), _ptr(S), _ptr(table), _ptr(buckets), _ptr(mask), C.byref(geom), scale, p, seed, _dt(S),
-                                          _dt(table), _ptr(dS), _ptr(dtable), wp, wb, _stream()), "hlq_rel_softmax_backward")
+    _check((_lib or lib()).hlq_rel_softmax_backward(
+        _dense("dP", dP, n, dt), s, t, b, m, C.byref(geom), scale, p, seed, _dtype_code(dt), _dtype_code(tdt), _dense("dS", dS, n, dt),
+        _dense("dtable", dtable, nt, tdt), wp, wb, _stream()), "hlq_rel_softmax_backward")

@@ -85,6 +85,64 @@ template <> struct Raw<float, 1> {
     static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
 };
 
+// ---- the same by buffer instructions ---------------------------------------------------------
+// A place beyond the buffer's bytes loads zeros and stores nothing, so the lanes with nothing to do need no branch: a place with kNowhere ored
+// in is beyond every buffer.
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p, int bytes = 0x7FFFFFFF)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ void buffer_load(Raw<bf16_t, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0); }
+__device__ __forceinline__ void buffer_load(Raw<float, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at)
+{
+    r.a = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
+    r.b = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at + 16, 0, 0));
+}
+__device__ __forceinline__ void buffer_load(Raw<bf16_t, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0); }
+__device__ __forceinline__ void buffer_load(Raw<float, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_bit_cast(f2_t, __builtin_amdgcn_raw_buffer_load_b64(b, at, 0, 0)); }
+__device__ __forceinline__ void buffer_load(Raw<bf16_t, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0); }
+__device__ __forceinline__ void buffer_load(Raw<float, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0)); }
+
+template <typename T, int NE> struct BufferStore;
+template <> struct BufferStore<bf16_t, 8> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
+    {
+        raw4_t o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
+    }
+};
+template <> struct BufferStore<float, 8> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
+    {
+        raw4_t o, q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[i]), q[i] = __float_as_uint(v[4 + i]);
+        __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(q, b, at + 16, 0, 0);
+    }
+};
+template <> struct BufferStore<bf16_t, 2> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v) { __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(v[0], v[1]), b, at, 0, 0); }
+};
+template <> struct BufferStore<float, 2> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
+    {
+        __builtin_amdgcn_raw_buffer_store_b64(raw2_t{__float_as_uint(v[0]), __float_as_uint(v[1])}, b, at, 0, 0);
+    }
+};
+template <> struct BufferStore<bf16_t, 1> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
+    {
+        __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(pack_bf16(v[0], 0.0f) & 0xFFFFu), b, at, 0, 0);
+    }
+};
+template <> struct BufferStore<float, 1> {
+    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), b, at, 0, 0); }
+};
+
 template <typename T> __device__ __forceinline__ float load_one(const T *p)
 {
     float v;
@@ -99,6 +157,22 @@ template <typename T> __device__ __forceinline__ void store_one(T *p, float v) {
 __device__ __forceinline__ float load_param(const void *p, bool f32, int64_t i)
 {
     return f32 ? static_cast<const float *>(p)[i] : load_one(static_cast<const bf16_t *>(p) + i);
+}
+template <int NE>
+__device__ __forceinline__ void load_params(const void *p, bool f32, int64_t i, float otherwise, float *v)
+{
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) v[e] = otherwise;
+    } else if (f32) {
+        Raw<float, NE> r;
+        r.load(static_cast<const float *>(p) + i);
+        r.widen(v);
+    } else {
+        Raw<bf16_t, NE> r;
+        r.load(static_cast<const bf16_t *>(p) + i);
+        r.widen(v);
+    }
 }
 __device__ __forceinline__ void store_param(void *p, bool f32, int64_t i, float v)
 {
@@ -176,6 +250,58 @@ __device__ __forceinline__ void drop_values(float *v, int64_t i, const DropRule 
     }
 }
 
+// Zeros for the elements that dropout drops; what is kept is not scaled.  word: the first of the four words, a multiple of 4.
+// On bf16 two halves at a time: w - (below - 1) cut at 0 is 0 where dropped; adding 0xFFFE cut at 0xFFFF and taken from 0xFFFE it is the
+// mask.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void drop_raw(Raw<bf16_t, 8> &r, uint32_t word, const DropRule &d)
+{
+    uint32_t w[4];
+    rand_words<4>(word, d.k0, d.k1, w);
+    const uint32_t under = (d.below - 1) * 0x10001u, most = 0xFFFEFFFEu;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t m;
+        asm("v_pk_sub_u16 %0, %1, %2 clamp\n\tv_pk_add_u16 %0, %0, %3 clamp\n\tv_pk_sub_u16 %0, %3, %0" : "=&v"(m) : "v"(w[k]), "s"(under), "v"(most));
+        r.w[k] &= m;
+    }
+}
+__device__ __forceinline__ void drop_raw(Raw<float, 8> &r, uint32_t word, const DropRule &d)
+{
+    uint32_t w[4];
+    rand_words<4>(word, d.k0, d.k1, w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bool lo = (w[k] & 0xFFFFu) >= d.below, hi = (w[k] >> 16) >= d.below;
+        if (k < 2) {
+            r.a[2 * k] = lo ? r.a[2 * k] : 0.0f;
+            r.a[2 * k + 1] = hi ? r.a[2 * k + 1] : 0.0f;
+        } else {
+            r.b[2 * k - 4] = lo ? r.b[2 * k - 4] : 0.0f;
+            r.b[2 * k - 3] = hi ? r.b[2 * k - 3] : 0.0f;
+        }
+    }
+}
+// the same for vectors of 2 and 1, `i` the first element
+template <typename T> __device__ __forceinline__ void drop_raw(Raw<T, 2> &r, int64_t i, const DropRule &d)
+{
+    uint32_t w;
+    rand_words<1>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, &w);
+    const bool lo = (w & 0xFFFFu) >= d.below, hi = (w >> 16) >= d.below;
+    if constexpr (sizeof(T) == 2) {
+        r.w &= (lo ? 0xFFFFu : 0u) | (hi ? 0xFFFF0000u : 0u);
+    } else {
+        r.w[0] = lo ? r.w[0] : 0.0f;
+        r.w[1] = hi ? r.w[1] : 0.0f;
+    }
+}
+template <typename T> __device__ __forceinline__ void drop_raw(Raw<T, 1> &r, int64_t i, const DropRule &d)
+{
+    uint32_t w;
+    rand_words<1>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, &w);
+    r.w = (((i & 1) ? w >> 16 : w & 0xFFFFu) >= d.below) ? r.w : T{};
+}
+
 // ---- sums and maxima over aligned groups of LANES lanes of a wavefront ---------------------------
 // Steps of 1 and 2 are quad permutes, 4 and 8 mirrors of half rows and rows (after the smaller steps all lanes of a quad,
 // of a half row, hold the same); 16 and 32 swap rows and halves of two copies, which leaves the two values in two registers: no
@@ -201,6 +327,31 @@ template <int LANES, int STEP = 1> __device__ __forceinline__ float lanes_sum(fl
         return x;
     }
 }
+// Sum over the lanes of a wavefront that are congruent modulo `stride` (a power of two up to 64, the same for all lanes): rotations within
+// rows of 16, then the swaps.
+template <int NE> __device__ __forceinline__ void congruent_sums(float *v, int stride)
+{
+#define HLQ_ROTATE(STEP)                                                                                                                   \
+    if (stride <= STEP) {                                                                                                                  \
+        _Pragma("unroll") for (int e = 0; e < NE; ++e)                                                                                     \
+            v[e] += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v[e]), 0x120 + STEP, 0xF, 0xF, true)); \
+    }
+    HLQ_ROTATE(1)
+    HLQ_ROTATE(2)
+    HLQ_ROTATE(4)
+    HLQ_ROTATE(8)
+#undef HLQ_ROTATE
+    float lo, hi;
+    if (stride <= 16) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) lane_pair<16>(v[e], &lo, &hi), v[e] = lo + hi;
+    }
+    if (stride <= 32) {
+#pragma unroll
+        for (int e = 0; e < NE; ++e) lane_pair<32>(v[e], &lo, &hi), v[e] = lo + hi;
+    }
+}
+
 // The larger of x and its partner's in one instruction; written out, for fmaxf adds one that quiets the partner's value, which here is no
 // signalling NaN.  (s_nop: what the vector unit has just written, a permuted read sees two states later.)
 #define HLQ_MAX_DPP(CTRL) asm("s_nop 1\n\tv_max_f32_dpp %0, %1, %1 " CTRL " row_mask:0xf bank_mask:0xf bound_ctrl:1" : "=v"(r) : "v"(x))

@@ -1154,8 +1154,7 @@ size_t element_bytes(int dtype) { return dtype == HLQ_F32 ? 4 : 2; }
 int check_group_norm(int64_t Nb, int64_t P, int64_t C, int64_t groups)
 {
     if (Nb < 0 || P <= 0 || C <= 0 || groups <= 0 || C % groups != 0) return HLQ_ERR_SHAPE;
-    if (C > (int64_t(1) << 24) || P > (int64_t(1) << 40) / C || Nb >= (int64_t(1) << 31) / C) return HLQ_ERR_SHAPE;
-    if (Nb > 0 && P * C > (int64_t(1) << 48) / Nb) return HLQ_ERR_SHAPE;
+    if (C > (1 << 17) || P > (1 << 30) || Nb >= (int64_t(1) << 31) / C) return HLQ_ERR_SHAPE;
     if (!hlq::group_norm_ok(static_cast<int>(C), static_cast<int>(C / groups))) return HLQ_ERR_SHAPE;
     return HLQ_OK;
 }

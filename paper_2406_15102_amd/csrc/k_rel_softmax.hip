@@ -194,15 +194,6 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *base, int64_t at, i
     const uint64_t top = (((m & low) + low) | m) & ~low;               // bit 7 of every byte that is not zero
     return static_cast<uint32_t>((top >> 7) * 0x0102040810204080ull >> 56);
 }
-// ---- vectors of a row by buffer instructions: a lane with nothing to load or store has a place beyond the buffer's end ----------------
-constexpr uint32_t kNowhere = 0x80000000u;       // ored into a lane's place in bytes
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7FFFFFFF, 0x00020000); }
-__device__ __forceinline__ void buffer_load(Raw<bf16_t, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0); }
-__device__ __forceinline__ void buffer_load(Raw<float, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at)
-{
-    r.a = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
-    r.b = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 16, 0));
-}
 // v[0 .. 8) to `at` where k0 + 8 <= K; the lane whose eight the row's end cuts stores the K % 8 it has (`cut`: its place, others kNowhere).
 // One store for sure, and others only where K % 8 is not 0: the wait for the loads behind it need not wait for it.
 __device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail, const float *v, bf16_t)
@@ -251,39 +242,6 @@ __device__ __forceinline__ void keep_bits(Raw<float, 8> &r, uint32_t bits)
         r.b[i] = (bits >> (4 + i)) & 1 ? r.b[i] : 0.0f;
     }
 }
-// Zeros for the elements that dropout drops; what is kept is not scaled.  word: the first of the four words, a multiple of 4.
-// On bf16 two halves at a time: w - (below - 1) cut at 0 is 0 where dropped; adding 0xFFFE cut at 0xFFFF and taken from 0xFFFE it is the
-// mask.
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void drop_raw(Raw<bf16_t, 8> &r, uint32_t word, const DropRule &d)
-{
-    uint32_t w[4];
-    rand_words<4>(word, d.k0, d.k1, w);
-    const uint32_t under = (d.below - 1) * 0x10001u, most = 0xFFFEFFFEu;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t m;
-        asm("v_pk_sub_u16 %0, %1, %2 clamp\n\tv_pk_add_u16 %0, %0, %3 clamp\n\tv_pk_sub_u16 %0, %3, %0" : "=&v"(m) : "v"(w[k]), "s"(under), "v"(most));
-        r.w[k] &= m;
-    }
-}
-__device__ __forceinline__ void drop_raw(Raw<float, 8> &r, uint32_t word, const DropRule &d)
-{
-    uint32_t w[4];
-    rand_words<4>(word, d.k0, d.k1, w);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const bool lo = (w[k] & 0xFFFFu) >= d.below, hi = (w[k] >> 16) >= d.below;
-        if (k < 2) {
-            r.a[2 * k] = lo ? r.a[2 * k] : 0.0f;
-            r.a[2 * k + 1] = hi ? r.a[2 * k + 1] : 0.0f;
-        } else {
-            r.b[2 * k - 4] = lo ? r.b[2 * k - 4] : 0.0f;
-            r.b[2 * k - 3] = hi ? r.b[2 * k - 3] : 0.0f;
-        }
-    }
-}
-
 // exp(z - top) of a row's scores.  On bf16 scores one fma and the base-2 exponential, of z l - top l with l = log2(e).  Where |top| is so
 // large that the product overflows, scores are either top or further from it than any exponential reaches: a small l tells as much.
 template <bool EXACT> struct RowExp {
