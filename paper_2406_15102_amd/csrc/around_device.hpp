@@ -29,13 +29,12 @@ template <> struct Raw<bf16_t, 8> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
     }
-    static __device__ __forceinline__ void store(bf16_t *p, const float *v)
+    __device__ __forceinline__ void pack(const float *v)
     {
-        raw4_t o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<raw4_e2 *>(p) = o;
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     }
+    __device__ __forceinline__ void store(bf16_t *p) const { *reinterpret_cast<raw4_e2 *>(p) = w; }
 };
 template <> struct Raw<float, 8> {
     f4_t a, b;
@@ -50,10 +49,15 @@ template <> struct Raw<float, 8> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
     }
-    static __device__ __forceinline__ void store(float *p, const float *v)
+    __device__ __forceinline__ void pack(const float *v)
     {
-        *reinterpret_cast<f4_e4 *>(p) = f4_t{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f4_e4 *>(p + 4) = f4_t{v[4], v[5], v[6], v[7]};
+        a = f4_t{v[0], v[1], v[2], v[3]};
+        b = f4_t{v[4], v[5], v[6], v[7]};
+    }
+    __device__ __forceinline__ void store(float *p) const
+    {
+        *reinterpret_cast<f4_e4 *>(p) = a;
+        *reinterpret_cast<f4_e4 *>(p + 4) = b;
     }
 };
 template <> struct Raw<bf16_t, 2> {
@@ -61,28 +65,30 @@ template <> struct Raw<bf16_t, 2> {
     __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const raw1_e2 *>(p); }
     __device__ __forceinline__ void zero() { w = 0; }
     __device__ __forceinline__ void widen(float *v) const { v[0] = bf16_lo(w), v[1] = bf16_hi(w); }
-    static __device__ __forceinline__ void store(bf16_t *p, const float *v) { *reinterpret_cast<raw1_e2 *>(p) = pack_bf16(v[0], v[1]); }
+    __device__ __forceinline__ void pack(const float *v) { w = pack_bf16(v[0], v[1]); }
 };
 template <> struct Raw<float, 2> {
     f2_t w;
     __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const f2_e4 *>(p); }
     __device__ __forceinline__ void zero() { w = f2_t{0.0f, 0.0f}; }
     __device__ __forceinline__ void widen(float *v) const { v[0] = w[0], v[1] = w[1]; }
-    static __device__ __forceinline__ void store(float *p, const float *v) { *reinterpret_cast<f2_e4 *>(p) = f2_t{v[0], v[1]}; }
+    __device__ __forceinline__ void pack(const float *v) { w = f2_t{v[0], v[1]}; }
 };
 template <> struct Raw<bf16_t, 1> {
     bf16_t w;
     __device__ __forceinline__ void load(const bf16_t *p) { w = *p; }
     __device__ __forceinline__ void zero() { w = 0; }
     __device__ __forceinline__ void widen(float *v) const { v[0] = bf16_lo(w); }
-    static __device__ __forceinline__ void store(bf16_t *p, const float *v) { *p = static_cast<bf16_t>(pack_bf16(v[0], 0.0f) & 0xFFFFu); }
+    __device__ __forceinline__ void pack(const float *v) { w = static_cast<bf16_t>(pack_bf16(v[0], 0.0f) & 0xFFFFu); }
+    __device__ __forceinline__ void store(bf16_t *p) const { *p = w; }
 };
 template <> struct Raw<float, 1> {
     float w;
     __device__ __forceinline__ void load(const float *p) { w = *p; }
     __device__ __forceinline__ void zero() { w = 0.0f; }
     __device__ __forceinline__ void widen(float *v) const { v[0] = w; }
-    static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
+    __device__ __forceinline__ void pack(const float *v) { w = v[0]; }
+    __device__ __forceinline__ void store(float *p) const { *p = w; }
 };
 
 // ---- the same by buffer instructions ---------------------------------------------------------
@@ -104,44 +110,16 @@ __device__ __forceinline__ void buffer_load(Raw<float, 2> &r, __amdgpu_buffer_rs
 __device__ __forceinline__ void buffer_load(Raw<bf16_t, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0); }
 __device__ __forceinline__ void buffer_load(Raw<float, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0)); }
 
-template <typename T, int NE> struct BufferStore;
-template <> struct BufferStore<bf16_t, 8> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
-    {
-        raw4_t o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
-    }
-};
-template <> struct BufferStore<float, 8> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
-    {
-        raw4_t o, q;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[i]), q[i] = __float_as_uint(v[4 + i]);
-        __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b128(q, b, at + 16, 0, 0);
-    }
-};
-template <> struct BufferStore<bf16_t, 2> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v) { __builtin_amdgcn_raw_buffer_store_b32(pack_bf16(v[0], v[1]), b, at, 0, 0); }
-};
-template <> struct BufferStore<float, 2> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
-    {
-        __builtin_amdgcn_raw_buffer_store_b64(raw2_t{__float_as_uint(v[0]), __float_as_uint(v[1])}, b, at, 0, 0);
-    }
-};
-template <> struct BufferStore<bf16_t, 1> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v)
-    {
-        __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(pack_bf16(v[0], 0.0f) & 0xFFFFu), b, at, 0, 0);
-    }
-};
-template <> struct BufferStore<float, 1> {
-    static __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t b, uint32_t at, const float *v) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), b, at, 0, 0); }
-};
+__device__ __forceinline__ void buffer_store(const Raw<bf16_t, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b128(r.w, b, at, 0, 0); }
+__device__ __forceinline__ void buffer_store(const Raw<float, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw4_t, r.a), b, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw4_t, r.b), b, at + 16, 0, 0);
+}
+__device__ __forceinline__ void buffer_store(const Raw<bf16_t, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b32(r.w, b, at, 0, 0); }
+__device__ __forceinline__ void buffer_store(const Raw<float, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(raw2_t, r.w), b, at, 0, 0); }
+__device__ __forceinline__ void buffer_store(const Raw<bf16_t, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b16(r.w, b, at, 0, 0); }
+__device__ __forceinline__ void buffer_store(const Raw<float, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r.w), b, at, 0, 0); }
 
 template <typename T> __device__ __forceinline__ float load_one(const T *p)
 {
@@ -151,7 +129,12 @@ template <typename T> __device__ __forceinline__ float load_one(const T *p)
     r.widen(&v);
     return v;
 }
-template <typename T> __device__ __forceinline__ void store_one(T *p, float v) { Raw<T, 1>::store(p, &v); }
+template <typename T> __device__ __forceinline__ void store_one(T *p, float v)
+{
+    Raw<T, 1> r;
+    r.pack(&v);
+    r.store(p);
+}
 
 // a layer's parameter, which has an element type of its own
 __device__ __forceinline__ float load_param(const void *p, bool f32, int64_t i)
@@ -190,6 +173,24 @@ template <bool EXACT> __device__ __forceinline__ float exp_of(float x)
 template <bool EXACT> __device__ __forceinline__ float recip_of(float x) { return EXACT ? 1.0f / x : __builtin_amdgcn_rcpf(x); }
 
 // ---- activations (HLQ_ACT_*) -------------------------------------------------------------------
+// Phi(z) of the normal distribution and exp(-z^2 / 2), which belongs to its slope.  EXACT by the error function.  Else by the rational
+// approximation of erfc in Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (error of erf at most 1.5e-7), which takes the same
+// exponential: a fifth of the error function's instructions.
+template <bool EXACT> __device__ __forceinline__ float normal_cdf(float z, float *bell)
+{
+    *bell = exp_of<EXACT>(-0.5f * z * z);
+    if constexpr (EXACT) {
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    } else {
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
+        float p = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+        p = __builtin_fmaf(t, p, 0.5f * 1.421413741f);
+        p = __builtin_fmaf(t, p, 0.5f * -0.284496736f);
+        p = __builtin_fmaf(t, p, 0.5f * 0.254829592f);
+        const float tail = p * t * *bell;                                    // Phi(-|z|)
+        return z < 0.0f ? tail : 1.0f - tail;
+    }
+}
 template <bool EXACT, int NE>
 __device__ __forceinline__ void act_values(float *z, int act)
 {
@@ -201,7 +202,10 @@ __device__ __forceinline__ void act_values(float *z, int act)
         for (int e = 0; e < NE; ++e) z[e] *= recip_of<EXACT>(1.0f + exp_of<EXACT>(-z[e]));
     } else if (act == 3) {
 #pragma unroll
-        for (int e = 0; e < NE; ++e) z[e] = 0.5f * z[e] * (1.0f + erff(z[e] * 0.70710678118654752f));
+        for (int e = 0; e < NE; ++e) {
+            float bell;
+            z[e] *= normal_cdf<EXACT>(z[e], &bell);
+        }
     }
 }
 // d[e] *= slope of the activation at z[e]
@@ -220,8 +224,9 @@ __device__ __forceinline__ void act_slopes(const float *z, int act, float *d)
     } else if (act == 3) {
 #pragma unroll
         for (int e = 0; e < NE; ++e) {
-            const float cdf = 0.5f * (1.0f + erff(z[e] * 0.70710678118654752f));
-            d[e] *= __builtin_fmaf(z[e] * 0.39894228040143268f, exp_of<EXACT>(-0.5f * z[e] * z[e]), cdf);
+            float bell;
+            const float cdf = normal_cdf<EXACT>(z[e], &bell);
+            d[e] *= __builtin_fmaf(z[e] * 0.39894228040143268f, bell, cdf);
         }
     }
 }
@@ -229,28 +234,9 @@ __device__ __forceinline__ void act_slopes(const float *z, int act, float *d)
 // ---- dropout -----------------------------------------------------------------------------------
 // Element i is dropped where half i & 1 (the low one first) of word i >> 1 of the stream is below `below` (= 65536 p rounded to
 // a whole number), else multiplied by `scale` = 65536 / (65536 - below).  below = 0: there is no dropout.
-// v[0 .. NE) are elements i .. i + NE - 1, i a multiple of NE (NE = 1, 2 or 8).  A dropped element is 0 whatever it was.
-template <int NE>
-__device__ __forceinline__ void drop_values(float *v, int64_t i, const DropRule &d)
-{
-    if constexpr (NE == 1) {
-        uint32_t w;
-        rand_words<1>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, &w);
-        const uint32_t u = (i & 1) ? w >> 16 : w & 0xFFFFu;
-        v[0] = u >= d.below ? v[0] * d.scale : 0.0f;
-    } else {
-        constexpr int NW = NE / 2;
-        uint32_t w[NW];
-        rand_words<NW>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, w);
-#pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            v[2 * k] = (w[k] & 0xFFFFu) >= d.below ? v[2 * k] * d.scale : 0.0f;
-            v[2 * k + 1] = (w[k] >> 16) >= d.below ? v[2 * k + 1] * d.scale : 0.0f;
-        }
-    }
-}
+// What is kept is multiplied by the operators themselves, where it often joins another factor.  A dropped element is 0 whatever it was.
 
-// Zeros for the elements that dropout drops; what is kept is not scaled.  word: the first of the four words, a multiple of 4.
+// zeros for the elements that dropout drops, of eight that take the four words from `word`, a multiple of 4, on
 // On bf16 two halves at a time: w - (below - 1) cut at 0 is 0 where dropped; adding 0xFFFE cut at 0xFFFF and taken from 0xFFFE it is the
 // mask.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));

@@ -11,6 +11,7 @@ template <typename T, bool RES, int U>
 __global__ __launch_bounds__(256) void k_dropout(const T *x, const T *r, int64_t n, DropRule d, T *y)
 {
     const int64_t base = (static_cast<int64_t>(blockIdx.x) * U * 256 + threadIdx.x) * 8;
+    const float factor = d.below ? d.scale : 1.0f;
     Raw<T, 8> a[U], b[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -25,18 +26,24 @@ __global__ __launch_bounds__(256) void k_dropout(const T *x, const T *r, int64_t
         const int64_t i = base + u * 2048;
         float v[8], q[8];
         if (i + 8 <= n) {
+            if (d.below) drop_raw(a[u], static_cast<uint32_t>(i >> 1), d);
             a[u].widen(v);
-            if (d.below) drop_values<8>(v, i, d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= factor;
             if (RES) {
                 b[u].widen(q);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += q[e];
             }
-            Raw<T, 8>::store(y + i, v);
+            a[u].pack(v);
+            a[u].store(y + i);
         } else {
             for (int64_t k = i; k < n; ++k) {          // at most seven, in one lane of the grid
-                v[0] = load_one(x + k);
-                if (d.below) drop_values<1>(v, k, d);
+                Raw<T, 1> one;
+                one.load(x + k);
+                if (d.below) drop_raw(one, k, d);
+                one.widen(v);
+                v[0] *= factor;
                 if (RES) v[0] += load_one(r + k);
                 store_one(y + k, v[0]);
             }

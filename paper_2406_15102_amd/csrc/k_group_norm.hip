@@ -50,8 +50,10 @@ GroupNormPlan plan_for(int64_t Nb, int64_t P, int C, int cg, bool is_f32, bool b
     int unit = 0;
     slab_unit(C, cg, &p.ve, &unit);
     const int want = kSlabBytes / (is_f32 ? 4 : 2);
-    int slab = (want + unit - 1) / unit * unit;
-    if (slab > C) slab = C;          // a multiple of the unit, too
+    // as many slabs of that size as there are, of equal size
+    const int units = C / unit, least = (want + unit - 1) / unit, most_slabs = units / least > 1 ? units / least : 1;
+    int slab = (units + most_slabs - 1) / most_slabs * unit;
+    if (slab > kMaxSlab || slab / p.ve > 1024) slab = least * unit < C ? least * unit : C;
     p.lanes = slab / p.ve;
     p.slabs = (C + slab - 1) / slab;
     p.aligned = p.lanes <= 64 && (p.lanes & (p.lanes - 1)) == 0;
@@ -246,16 +248,28 @@ __device__ __forceinline__ void of_groups(const float *table, int c, int cg, flo
 
 // ---- forward ----------------------------------------------------------------------------------
 
+template <typename T, int VE>
+__device__ __forceinline__ void drop_vector(Raw<T, VE> &r, int64_t at, const DropRule &d)
+{
+    if constexpr (VE == 8) drop_raw(r, static_cast<uint32_t>(at >> 1), d);
+    else drop_raw(r, at, d);
+}
+
 // y of a vector at element `at` of the tensor
 template <typename T, int VE>
-__device__ __forceinline__ void finish(const GroupNormArgs &a, const Raw<T, VE> &raw, const float *mean, const float *w, const float *b, int64_t at,
-                                       float *u)
+__device__ __forceinline__ void finish(const GroupNormArgs &a, Raw<T, VE> &raw, const float *mean, const float *w, const float *b, int64_t at)
 {
+    float u[VE];
     raw.widen(u);
 #pragma unroll
     for (int e = 0; e < VE; ++e) u[e] = __builtin_fmaf(u[e] - mean[e], w[e], b[e]);
     act_values<sizeof(T) == 4, VE>(u, a.act);
-    if (a.drop.below) drop_values<VE>(u, at, a.drop);
+    if (a.drop.below) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) u[e] *= a.drop.scale;
+    }
+    raw.pack(u);
+    if (a.drop.below) drop_vector(raw, at, a.drop);
 }
 
 // A slab's map in one tile of rows * NV positions.
@@ -324,8 +338,8 @@ __global__ __launch_bounds__(THREADS) void k_gn_tile(GroupNormArgs a, GroupNormP
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         if (j * s.rows < static_cast<int>(a.P)) {               // the same for the workgroup
-            finish<T, VE>(a, raw[j], mean, w, b, at + static_cast<int64_t>(j) * s.rows * a.C, u);
-            BufferStore<T, VE>::store(by, l.voff + j * l.step, u);
+            finish<T, VE>(a, raw[j], mean, w, b, at + static_cast<int64_t>(j) * s.rows * a.C);
+            buffer_store(raw[j], by, l.voff + j * l.step);
         }
     }
 }
@@ -430,9 +444,9 @@ __global__ __launch_bounds__(THREADS) void k_gn_apply(GroupNormArgs a, GroupNorm
         load_params<VE>(a.w, a.param_f32, s.c, 1.0f, w);
         load_params<VE>(a.b, a.param_f32, s.c, 0.0f, b);
     }
-    // three floats a thread: count, mean, squared distances of the chunks seg, seg + segs, ... of group g
-    float *ln = lds, *lm = lds + T_, *lq = lds + 2 * T_, *gm = lds + 3 * T_, *gr = gm + s.ncol;
-    const int segs = T_ / s.ng;
+    // thread (seg, g): the chunks seg, seg + segs, ... of group g joined; then the means of the group's threads, then the squared distances
+    float *lm = lds, *lq = lds + T_, *gm = lds + 2 * T_, *gr = gm + s.ncol;
+    const int segs = T_ / s.ng, used = segs < p.chunks ? segs : p.chunks;
     const int g = tid % s.ng, seg = tid / s.ng;
     const float2 *part = static_cast<const float2 *>(a.ws) + static_cast<int64_t>(s.img) * p.chunks * a.groups + s.c0 / a.cg;
     float n = 0.0f, mean = 0.0f, m2 = 0.0f;
@@ -441,24 +455,26 @@ __global__ __launch_bounds__(THREADS) void k_gn_apply(GroupNormArgs a, GroupNorm
             const float2 v = part[static_cast<int64_t>(k) * a.groups + g];
             const int64_t px = k + 1 < p.chunks ? p.chunk_px : a.P - static_cast<int64_t>(k) * p.chunk_px;
             const float nk = static_cast<float>(px) * static_cast<float>(a.cg), both = n + nk;
-            join(n, mean, m2, v.x, v.y, nk / both);
+            join(n, mean, m2, v.x, v.y, k == seg ? 1.0f : nk / both);
             n = both;
         }
     }
-    ln[tid] = n, lm[tid] = mean, lq[tid] = m2;
+    const float inv_n = 1.0f / (static_cast<float>(a.P) * static_cast<float>(a.cg));
+    lm[tid] = n * mean;
+    __syncthreads();
+    float all = 0.0f;
+    for (int k = 0; k < used; ++k) all += lm[k * s.ng + g];
+    all *= inv_n;
+    lq[tid] = __builtin_fmaf(n * (mean - all), mean - all, m2);
     __syncthreads();
     if (tid < s.ng) {
-        for (int k = 1; k < segs && k < p.chunks; ++k) {
-            const int o = k * s.ng + tid;
-            const float both = n + ln[o];
-            join(n, mean, m2, lm[o], lq[o], ln[o] / both);
-            n = both;
-        }
-        const float r = 1.0f / sqrtf(m2 / n + a.eps);
-        gm[tid] = mean, gr[tid] = r;
+        float q2 = 0.0f;
+        for (int k = 0; k < used; ++k) q2 += lq[k * s.ng + tid];
+        const float r = 1.0f / sqrtf(__builtin_fmaf(q2, inv_n, a.eps));
+        gm[tid] = all, gr[tid] = r;
         if (s.chunk == 0) {
             const int64_t o = static_cast<int64_t>(s.img) * a.groups + s.c0 / a.cg + tid;
-            if (a.mean) a.mean[o] = mean;
+            if (a.mean) a.mean[o] = all;
             if (a.rstd) a.rstd[o] = r;
         }
     }
@@ -479,8 +495,8 @@ __global__ __launch_bounds__(THREADS) void k_gn_apply(GroupNormArgs a, GroupNorm
         const int64_t at = l.first + s.row * a.C + s.lane * VE;
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            finish<T, VE>(a, raw[j], mu, w, b, at + static_cast<int64_t>(j) * s.rows * a.C, u);
-            BufferStore<T, VE>::store(by, l.voff + j * l.step, u);
+            finish<T, VE>(a, raw[j], mu, w, b, at + static_cast<int64_t>(j) * s.rows * a.C);
+            buffer_store(raw[j], by, l.voff + j * l.step);
         }
     }
 }
@@ -515,10 +531,7 @@ template <int VE> struct Channels {
     {
         float z[VE];
         x.widen(d);
-        if (g.drop.below) {
-            if constexpr (VE == 8) drop_raw(dy, static_cast<uint32_t>(at >> 1), g.drop);
-            else drop_raw(dy, at, g.drop);
-        }
+        if (g.drop.below) drop_vector(dy, at, g.drop);
         dy.widen(dz);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
@@ -612,7 +625,8 @@ __global__ __launch_bounds__(THREADS) void k_gn_grad_tile(GroupNormArgs a, Group
             x[j].widen(d);
 #pragma unroll
             for (int e = 0; e < VE; ++e) d[e] = __builtin_fmaf(dz[j][e], ch.a[e], -__builtin_fmaf(d[e] - ch.mean[e], c1[e], c0[e]));
-            BufferStore<T, VE>::store(by, l.voff + j * l.step, d);
+            x[j].pack(d);
+            buffer_store(x[j], by, l.voff + j * l.step);
         }
     }
 }
@@ -775,7 +789,9 @@ __global__ __launch_bounds__(THREADS) void k_gn_grad_apply(GroupNormArgs a, Grou
             ch.slope(a, x[j], dy[j], at + static_cast<int64_t>(j) * s.rows * a.C, d, dz);
 #pragma unroll
             for (int e = 0; e < VE; ++e) d[e] = __builtin_fmaf(dz[e], a_kept[e], -__builtin_fmaf(d[e], c1[e], c0[e]));
-            BufferStore<T, VE>::store(by, l.voff + j * l.step, d);
+            Raw<T, VE> o;
+            o.pack(d);
+            buffer_store(o, by, l.voff + j * l.step);
         }
     });
 }
@@ -815,7 +831,7 @@ static hipError_t forward(const GroupNormArgs &a, const GroupNormPlan &p, hipStr
     }
     k_gn_stats<T, VE, 4, THREADS><<<blocks, p.threads, lds, st>>>(a, p);
     if (const hipError_t e = hipGetLastError()) return e;
-    const size_t lds2 = sizeof(float) * (3 * p.threads + 2 * p.lanes * VE);
+    const size_t lds2 = sizeof(float) * (2 * p.threads + 2 * p.lanes * VE);
     if (far) k_gn_apply<T, VE, UL, THREADS><<<blocks, p.threads, lds2, st>>>(a, p);
     else k_gn_apply<T, VE, U, THREADS><<<blocks, p.threads, lds2, st>>>(a, p);
     return hipGetLastError();

@@ -17,11 +17,6 @@
 
 #include <algorithm>
 
-#ifndef LONG_AHEAD
-#define LONG_AHEAD false
-#define L2048 64
-#define LONG_WAVES 2
-#endif
 namespace hlq {
 
 // Where keys and queries lie: rel(q, k) = u(k) - u(q) + base.  Lines of a grid by a multiplication: exact for places below 2^16, of which a
@@ -46,6 +41,7 @@ struct RelMap {
 
 struct RelPlan {
     RelMap map;
+    bool batch;                  // k_rel_rows
     int lanes, nv;               // lanes of a row, vectors of 8 keys a lane
     int rows_q, rows_b;          // queries and batches that a workgroup's rows are in one step
     int q_block, q_blocks;       // queries of a workgroup
@@ -78,24 +74,22 @@ RelMap rel_map(const RelArgs &a)
 __host__ __device__ __forceinline__ int padded(int i) { return i + (i >> 3); }
 
 // workgroups that a compute unit holds at once, by registers and LDS
-int rel_resident(const RelPlan &p, bool back) { return back ? (p.lanes < 64 ? 5 : p.lanes < 256 ? 3 : 6) : 7; }
-#ifndef KSETUP
-#define KSETUP 5
-#define KCOVER 3
-#endif
-constexpr int64_t kSetup = KSETUP, kCover = KCOVER;
+int rel_resident(const RelPlan &p, bool back) { return back ? (p.batch ? (p.nv == 1 ? 5 : 3) : p.lanes < 256 ? 3 : 6) : 7; }
+constexpr int64_t kSetup = 5, kCover = 3;
 
 RelPlan rel_plan(const RelArgs &a, bool back)
 {
     RelPlan p{};
     p.map = rel_map(a);
     const int gw = p.map.w;
+    // Rows through the batch (k_rel_rows) up to 1024 keys where there is a batch to go through, else a row at a time.
+    p.batch = a.K <= 256 || (a.K <= 1024 && a.B >= 4);
     if (a.K <= 64) p.lanes = 8, p.nv = 1;
     else if (a.K <= 128) p.lanes = 16, p.nv = 1;
     else if (a.K <= 256) p.lanes = 32, p.nv = 1;
-    else if (a.K <= 512) p.lanes = 64, p.nv = 1;
+    else if (a.K <= 512) p.lanes = p.batch ? 32 : 64, p.nv = p.batch ? 2 : 1;
     else if (a.K <= 1024) p.lanes = 64, p.nv = 2;
-    else if (a.K <= 2048) p.lanes = L2048, p.nv = 256 / p.lanes;
+    else if (a.K <= 2048) p.lanes = 64, p.nv = 4;
     else if (a.K <= 4096) p.lanes = 256, p.nv = 2;
     else if (a.K <= 8192) p.lanes = 256, p.nv = 4;
     else p.lanes = 256, p.nv = 8;
@@ -143,14 +137,14 @@ RelPlan rel_plan(const RelArgs &a, bool back)
 // A sequence's vectors have room for every place that a row's lanes may reach, keys or not.
 __host__ __device__ __forceinline__ int rel_vector(const RelPlan &p)
 {
-    return p.lanes >= 64 && !p.map.w ? padded(p.lanes * p.nv * 8 + p.q_block) : p.win;
+    return !p.batch && !p.map.w ? padded(p.lanes * p.nv * 8 + p.q_block) : p.win;
 }
 size_t rel_lds_bytes(const RelPlan &p, bool back)
 {
     const size_t v = rel_vector(p);
     const int rows = kThreads / p.lanes;
     size_t n = v + 16 + (back && p.few ? (p.win + 3) / 4 : 0);
-    if (back) n += p.lanes == 64 ? 4 * v : v + (rows > 1 ? static_cast<size_t>(rows) * p.lanes * p.nv * 8 : 0);
+    if (back) n += p.batch ? v + static_cast<size_t>(rows) * p.lanes * p.nv * 8 : p.lanes == 64 ? 4 * v : v;
     return sizeof(float) * n;
 }
 
@@ -194,14 +188,12 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *base, int64_t at, i
     const uint64_t top = (((m & low) + low) | m) & ~low;               // bit 7 of every byte that is not zero
     return static_cast<uint32_t>((top >> 7) * 0x0102040810204080ull >> 56);
 }
-// v[0 .. 8) to `at` where k0 + 8 <= K; the lane whose eight the row's end cuts stores the K % 8 it has (`cut`: its place, others kNowhere).
+// A row's eight to `at` where k0 + 8 <= K; the lane whose eight the row's end cuts stores the K % 8 it has (`cut`: its place, others kNowhere).
 // One store for sure, and others only where K % 8 is not 0: the wait for the loads behind it need not wait for it.
-__device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail, const float *v, bf16_t)
+__device__ __forceinline__ void store_row(const Raw<bf16_t, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail)
 {
-    raw4_t o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-    __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
+    const raw4_t o = r.w;
+    buffer_store(r, b, at);
     if (tail) {
         if (tail & 4) __builtin_amdgcn_raw_buffer_store_b64(raw2_t{o[0], o[1]}, b, cut, 0, 0);
         const uint32_t two = tail & 4 ? o[2] : o[0], one = tail & 4 ? (tail & 2 ? o[3] : o[2]) : (tail & 2 ? o[1] : o[0]);
@@ -209,14 +201,11 @@ __device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at,
         if (tail & 1) __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(one), b, cut, (tail & 6) * 2, 0);
     }
 }
-__device__ __forceinline__ void store_row(__amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail, const float *v, float)
+__device__ __forceinline__ void store_row(const Raw<float, 8> &r, __amdgpu_buffer_rsrc_t b, uint32_t at, uint32_t cut, int tail)
 {
-    raw4_t o, q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[i]), q[i] = __float_as_uint(v[4 + i]);
-    __builtin_amdgcn_raw_buffer_store_b128(o, b, at, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(q, b, at, 16, 0);
+    buffer_store(r, b, at);
     if (tail) {
+        const raw4_t o = __builtin_bit_cast(raw4_t, r.a), q = __builtin_bit_cast(raw4_t, r.b);
         if (tail & 4) __builtin_amdgcn_raw_buffer_store_b128(o, b, cut, 0, 0);
         const uint32_t t0 = tail & 4 ? q[0] : o[0], t1 = tail & 4 ? q[1] : o[1];
         const uint32_t one = tail & 4 ? (tail & 2 ? q[2] : q[0]) : (tail & 2 ? o[2] : o[0]);
@@ -424,7 +413,7 @@ __device__ __forceinline__ void rel_write_sums(const RelArgs &a, const RelPlan &
 template <typename T> struct LaneMask;
 template <> struct LaneMask<bf16_t> {
     uint32_t m[4];
-    __device__ __forceinline__ explicit LaneMask(uint32_t bits)
+    __device__ __forceinline__ void set(uint32_t bits)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m[i] = ((bits >> (2 * i)) & 1u ? 0xFFFFu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xFFFF0000u : 0u);
@@ -437,7 +426,7 @@ template <> struct LaneMask<bf16_t> {
 };
 template <> struct LaneMask<float> {
     bool in[8];
-    __device__ __forceinline__ explicit LaneMask(uint32_t bits)
+    __device__ __forceinline__ void set(uint32_t bits)
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) in[i] = (bits >> i) & 1u;
@@ -452,18 +441,18 @@ template <> struct LaneMask<float> {
     }
 };
 
-// Rows of up to 256 keys, 8, 16 or 32 lanes each: several to a wavefront.  A query's bias stays in registers through the batch, minus infinity for
-// the keys that the query does not see, and so do the sums over the batch, which then meet in LDS: a thread sums those of one relative
-// position.  The next batch's row is fetched before the current one is worked on.  A place in memory is one of the whole workgroup's
-// (in scalar registers) and the lane's, which stays: rows_b is chosen so that the latter fits 32 bits.
-template <typename T, int LANES, bool BACK>
+// Rows of a few lanes, several to a wavefront (64 lanes: one), and a batch to go through: a query's bias stays in registers through the batch,
+// minus infinity for the keys that the query does not see, and so do the sums over the batch, which then meet in LDS: a thread sums those
+// of one relative position.  The next batch's row is fetched before the current one is worked on.  A place in memory is one of the whole
+// workgroup's (in scalar registers) and the lane's, which stays: rows_b is chosen so that the latter fits 32 bits.
+template <typename T, int LANES, int NV, bool BACK>
 __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
 {
     extern __shared__ float lds[];
     constexpr bool EXACT = sizeof(T) == 4;
-    constexpr int ROWS = kThreads / LANES, WIDTH = LANES * 8;
+    constexpr int ROWS = kThreads / LANES, STEP = LANES * 8, WIDTH = STEP * NV, NE = 8 * NV;
     const float NONE = -__builtin_inff();
-    const int tid = threadIdx.x, row = tid / LANES, lane = tid % LANES, k0 = lane * 8;
+    const int tid = threadIdx.x, row = tid / LANES, first = tid % LANES * 8;
     const RelJob job = rel_job(a, p);
     const int gw = p.map.w;
     float *bias = lds, *accw = bias + p.win, *tile = accw + (BACK ? p.win : 0);
@@ -471,32 +460,38 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
     const int64_t plane = static_cast<int64_t>(a.H) * a.Q * a.K, total = a.B * plane, mask_total = static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K;
     const int Kp = (a.K + 7) & ~7;
     const int row_q = row % p.rows_q, row_b = row / p.rows_q;
-    const uint32_t mine = (static_cast<uint32_t>(row_b * plane) + row_q * a.K + k0) * sizeof(T);      // the lane's place beside the workgroup's
+    const uint32_t mine = (static_cast<uint32_t>(row_b * plane) + row_q * a.K + first) * sizeof(T);   // the lane's place beside the workgroup's
     const int tail = a.K & 7;
-    // places of a whole vector and of one that the row's end cuts
-    const uint32_t at_whole = k0 + 8 <= a.K ? mine : kNowhere, at_cut = k0 < a.K && k0 + 8 > a.K ? mine : kNowhere;
-    const uint32_t word0 = static_cast<uint32_t>((((static_cast<int64_t>(row_b) * a.H) * a.Q + row_q) * Kp + k0) >> 1);      // of the random stream
+    const uint32_t word0 = static_cast<uint32_t>((((static_cast<int64_t>(row_b) * a.H) * a.Q + row_q) * Kp + first) >> 1);      // of the random stream
     const int64_t reach = (p.rows_b - 1) * plane + (p.rows_q - 1) * a.K + WIDTH;              // the workgroup's end beside its place
-    const float keep = BACK && a.drop.below ? a.drop.scale : 1.0f;
-    Raw<T, 8> ns, nd;
-    uint32_t nbits = 0xFFu;
+    const float keep = a.drop.below ? a.drop.scale : 1.0f;
+    Raw<T, 8> ns[NV], nd[NV];
+    uint32_t nbits[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) nbits[j] = 0xFFu;
     auto fetch = [&](int qs, int bs) {
         const int q = qs + row_q, b = bs + row_b;
         const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
         const int end = q < job.q1 && b < job.b1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
-        if (base + reach <= total) {
-            const uint32_t at = k0 < end ? mine : kNowhere;
-            buffer_load(ns, buffer_at(static_cast<const T *>(a.s) + base), at);
-            if (BACK) buffer_load(nd, buffer_at(static_cast<const T *>(a.dp) + base), at);
-        } else if (k0 < end) {                                    // the tensor's last rows
-            load_inside(ns, static_cast<const T *>(a.s), base + mine / sizeof(T), total);
-            if (BACK) load_inside(nd, static_cast<const T *>(a.dp), base + mine / sizeof(T), total);
-        } else {
-            ns.zero();
-            if (BACK) nd.zero();
+        const __amdgpu_buffer_rsrc_t rs = buffer_at(static_cast<const T *>(a.s) + base), rd = buffer_at(static_cast<const T *>(a.dp) + base);
+        const bool inside = base + reach <= total;                // else the tensor's last rows are among them
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int k0 = first + STEP * j;
+            if (inside) {
+                const uint32_t at = k0 < end ? mine + STEP * sizeof(T) * j : kNowhere;
+                buffer_load(ns[j], rs, at);
+                if (BACK) buffer_load(nd[j], rd, at);
+            } else if (k0 < end) {
+                load_inside(ns[j], static_cast<const T *>(a.s), base + mine / sizeof(T) + STEP * j, total);
+                if (BACK) load_inside(nd[j], static_cast<const T *>(a.dp), base + mine / sizeof(T) + STEP * j, total);
+            } else {
+                ns[j].zero();
+                if (BACK) nd[j].zero();
+            }
+            if (a.mask && k0 < end)
+                nbits[j] = load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0, mask_total);
         }
-        if (a.mask && k0 < end)
-            nbits = load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0, mask_total);
     };
     fetch(job.q0, job.b0);
     if (BACK)
@@ -506,45 +501,59 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
     for (int qs = job.q0; qs < job.q1; qs += p.rows_q) {
         const int q = qs + row_q;
         const int end = q < job.q1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
-        const uint32_t bits = end - k0 >= 8 ? 0xFFu : end > k0 ? (1u << (end - k0)) - 1u : 0u;
-        const LaneMask<T> inside(bits);
-        const bool whole = __all(bits == 0xFFu);
-        float bv[8], acc[8];
-        {
+        auto bits_of = [&](int j) {
+            const int left = end - first - STEP * j;
+            return left >= 8 ? 0xFFu : left > 0 ? (1u << left) - 1u : 0u;
+        };
+        LaneMask<T> inside[NV];
+        bool whole = true;
+        float bv[NE], acc[NE];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t bits = bits_of(j);
+            inside[j].set(bits);
+            whole = whole && bits == 0xFFu;
+            const int k0 = first + STEP * j;
             int i = p.map.u(k0) + p.map.base - p.map.u(q < job.q1 ? q : job.q1 - 1) - job.rlo, kx = gw ? p.map.column(k0) : 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                bv[e] = (bits >> e) & 1u ? bias[i] : NONE;
-                acc[e] = 0.0f;
+                bv[8 * j + e] = (bits >> e) & 1u ? bias[i] : NONE;
+                acc[8 * j + e] = 0.0f;
                 ++i;
                 if (gw && ++kx == gw) kx = 0, i += gw - 1;
             }
         }
+        whole = __all(whole);
         for (int bs = job.b0; bs < job.b1; bs += p.rows_b) {
-            Raw<T, 8> rs = ns, rd = nd;
-            const uint32_t seen = nbits;
+            Raw<T, 8> rs[NV], rd[NV];
+            uint32_t seen[NV];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) rs[j] = ns[j], rd[j] = nd[j], seen[j] = nbits[j];
             const bool same = bs + p.rows_b < job.b1;
             fetch(same ? qs : qs + p.rows_q, same ? bs + p.rows_b : job.b0);       // behind the last there is nothing to load
             const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
             const bool on = bs + row_b < job.b1 && q < job.q1;
-            if (!whole) {
-                inside(rs);
-                if (BACK) inside(rd);
+            float z[NE], sum = 0.0f, top = NONE;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (!whole) {
+                    inside[j](rs[j]);
+                    if (BACK) inside[j](rd[j]);
+                }
+                rs[j].widen(z + 8 * j);
+#pragma unroll
+                for (int e = 8 * j; e < 8 * j + 8; ++e) z[e] = __builtin_fmaf(z[e], a.scale, bv[e]);
+                if (a.mask) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[8 * j + e] = (seen[j] >> e) & 1u ? z[8 * j + e] : NONE;
+                    if (BACK) keep_bits(rd[j], seen[j]);               // whatever stands where nothing is seen
+                }
             }
-            float z[8], sum = 0.0f, top = NONE;
-            rs.widen(z);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = __builtin_fmaf(z[e], a.scale, bv[e]);
-            if (a.mask) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = (seen >> e) & 1u ? z[e] : NONE;
-                if (BACK) keep_bits(rd, seen);                         // whatever stands where nothing is seen
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, z[e]);
+            for (int e = 0; e < NE; ++e) top = fmaxf(top, z[e]);
             const RowExp<EXACT> exp_row(lanes_max<LANES>(top));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < NE; ++e) {
                 z[e] = exp_row(z[e]);
                 sum += z[e];
             }
@@ -553,32 +562,50 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
             const __amdgpu_buffer_rsrc_t out = buffer_at(static_cast<T *>(a.out) + base);
             const uint32_t off = on ? 0u : kNowhere;
             const uint32_t word = word0 + static_cast<uint32_t>((((static_cast<int64_t>(bs) * a.H + job.h) * a.Q + qs) * Kp) >> 1);
+            auto store = [&](int j, const Raw<T, 8> &v) {
+                // places of a whole vector and of one that the row's end cuts
+                const int k0 = first + STEP * j;
+                const uint32_t at = (mine + STEP * sizeof(T) * j) | off;
+                store_row(v, out, k0 + 8 <= a.K ? at : kNowhere, k0 < a.K && k0 + 8 > a.K ? at : kNowhere, tail);
+            };
             if constexpr (!BACK) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] *= inv;
-                if (a.drop.below) drop_values<8>(z, static_cast<int64_t>(word) * 2, a.drop);
-                store_row(out, at_whole | off, at_cut | off, tail, z, T{});
+                for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                    for (int e = 8 * j; e < 8 * j + 8; ++e) z[e] *= keep * inv;
+                    rs[j].pack(z + 8 * j);
+                    if (a.drop.below) drop_raw(rs[j], word + STEP / 2 * j, a.drop);
+                    store(j, rs[j]);
+                }
             } else {
                 float d[8], dot = 0.0f;
-                if (a.drop.below) drop_raw(rd, word, a.drop);
-                rd.widen(d);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(z[e], d[e], dot);
+                for (int j = 0; j < NV; ++j) {
+                    if (a.drop.below) drop_raw(rd[j], word + STEP / 2 * j, a.drop);
+                    rd[j].widen(d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(z[8 * j + e], d[e], dot);
+                }
                 dot = lanes_sum<LANES>(dot);
                 // z holds p / inv, d holds dp / keep, dot their product's sum:  dz = p (dp - sum p dp)
                 const float gain = on ? keep * inv : 0.0f, minus = on ? -(dot * inv) * gain : 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float dz = z[e] * __builtin_fmaf(d[e], gain, minus);
-                    acc[e] += dz;
-                    d[e] = dz * a.scale;
+                for (int j = 0; j < NV; ++j) {
+                    rd[j].widen(d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float dz = z[8 * j + e] * __builtin_fmaf(d[e], gain, minus);
+                        acc[8 * j + e] += dz;
+                        d[e] = dz * a.scale;
+                    }
+                    rd[j].pack(d);
+                    store(j, rd[j]);
                 }
-                store_row(out, at_whole | off, at_cut | off, tail, d, T{});
             }
         }
         if constexpr (BACK) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tile[row * WIDTH + k0 + e] = acc[e];
+            for (int e = 0; e < NE; ++e) tile[row * WIDTH + STEP * (e / 8) + first + e % 8] = acc[e];
             __syncthreads();
             const int qe = min(job.q1, qs + p.rows_q);
             const int i0 = p.map.first(qe) - job.rlo, i1 = p.map.last(qs) - job.rlo;
@@ -610,9 +637,9 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
 // Longer rows: a wavefront's (LANES = 64), or a workgroup's (LANES = 256).  The bias is read from LDS for every row, and a row's gradient
 // of the bias is added to LDS at once, to the wavefront's own vector or, where the workgroup is one row, to the one: a
 // row's relative positions are distinct, rows follow one another, so every sum has its order.  (Plain reads and writes: the same with
-// LDS atomics took 682 us for 2048 tokens and 32 heads where this took 217.)  AHEAD: the next row is fetched before the current is worked on.
-template <typename T, int LANES, int NV, bool GRID, bool BACK, bool AHEAD, int MINW>
-__global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan p)
+// LDS atomics took 682 us for 2048 tokens and 32 heads where this took 217.)
+template <typename T, int LANES, int NV, bool GRID, bool BACK>
+__global__ __launch_bounds__(kThreads, NV >= 8 ? 1 : 2) void k_rel_long(RelArgs a, RelPlan p)
 {
     extern __shared__ float lds[];
     constexpr bool EXACT = sizeof(T) == 4, WIDE = LANES == kThreads;
@@ -629,7 +656,7 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
     // the same for a whole wavefront
     const int row_q = __builtin_amdgcn_readfirstlane(row % p.rows_q), row_b = __builtin_amdgcn_readfirstlane(row / p.rows_q);
     const int wave_first = __builtin_amdgcn_readfirstlane(first);
-    const float keep = BACK && a.drop.below ? a.drop.scale : 1.0f;
+    const float keep = a.drop.below ? a.drop.scale : 1.0f;
     float *mine = sums + (WIDE ? 0 : (tid >> 6) * size);
     auto end_of = [&](int q, int b) {
         return q < job.q1 && b < job.b1 ? (a.causal ? min(a.K, q + a.K - a.Q + 1) : a.K) : 0;
@@ -652,12 +679,6 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
             for (int e = 0; e < 8; ++e) f(e, at + padded(shift + e) + padded(STEP) * j);
         }
     };
-    RelRow<T, NV, BACK> next;
-    auto fetch = [&](int qs, int bs) {
-        const int q = qs + row_q, b = bs + row_b;
-        next.load(a, ((static_cast<int64_t>(b) * a.H + job.h) * a.Q + q) * a.K, b, q, first, LANES, end_of(q, b), total);
-    };
-    if constexpr (AHEAD) fetch(job.q0, job.b0);
     for (int i = tid; i < VECTORS * size; i += kThreads) sums[i] = 0.0f;
     rel_fill(a, p, job, bias, ids, [](int i) { return GRID ? i : padded(i); });
     __syncthreads();
@@ -668,12 +689,8 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
             const bool on = b < job.b1 && q < job.q1;
             const int64_t line = (static_cast<int64_t>(b) * a.H + job.h) * a.Q + q;
             const int end = end_of(q, b);            // a wavefront passes over its vectors from here on
-            if constexpr (!AHEAD) fetch(qs, bs);
-            RelRow<T, NV, BACK> r = next;
-            if constexpr (AHEAD) {
-                const bool same = bs + p.rows_b < job.b1;
-                fetch(same ? qs : qs + p.rows_q, same ? bs + p.rows_b : job.b0);       // behind the last there is nothing to load
-            }
+            RelRow<T, NV, BACK> r;
+            r.load(a, line * a.K, b, q, first, LANES, end, total);
             float z[8 * NV], top = NONE, sum = 0.0f, v[8];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -732,10 +749,11 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
                     for (int e = 0; e < 8; ++e) v[e] = 0.0f;
                     if (wave_first + STEP * j < end) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = z[8 * j + e] * inv;
-                        if (a.drop.below) drop_values<8>(v, line * Kp + k0, a.drop);
+                        for (int e = 0; e < 8; ++e) v[e] = z[8 * j + e] * (keep * inv);
                     }
-                    store_row(out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail, v, T{});
+                    r.s[j].pack(v);
+                    if (a.drop.below && wave_first + STEP * j < end) drop_raw(r.s[j], static_cast<uint32_t>((line * Kp + k0) >> 1), a.drop);
+                    store_row(r.s[j], out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail);
                 }
             } else {
                 float dot = 0.0f, d[8];
@@ -784,7 +802,8 @@ __global__ __launch_bounds__(kThreads, MINW) void k_rel_long(RelArgs a, RelPlan 
 #pragma unroll
                         for (int e = 0; e < 8; ++e) d[e] = 0.0f;
                     }
-                    store_row(out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail, d, T{});
+                    r.d[j].pack(d);
+                    store_row(r.d[j], out, k0 + 8 <= a.K ? place : kNowhere, k0 < a.K && k0 + 8 > a.K ? place : kNowhere, tail);
                 }
             }
         }
@@ -826,18 +845,21 @@ __global__ __launch_bounds__(1024) void k_rel_few_buckets(RelArgs a, RelPlan p)
     }
 }
 
-// The same for many buckets, 64 of them from 64 * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
-// belong to the 64 buckets are listed in their order, 1024 at a time; 64 of the list go through the workgroups' vectors together, a wavefront
-// to every 16th vector, and then to their buckets, a lane each.
+// The same for many buckets, 16 of them from 16 * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
+// belong to the 16 buckets are listed in their order, 1024 at a time; 16 of the list go through the workgroups' vectors together, a quarter
+// of a wavefront to every 64th vector, and then to their buckets, a lane each.
+constexpr int kBuckets = 16;
 __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel)
 {
     __shared__ int list[1024], of[1024], count[16], owner[64];
-    __shared__ float part[16][64];
+    __shared__ float part[16][kBuckets];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = blockIdx.y;
-    const int c0 = blockIdx.x * 64, c1 = min(a.n_buckets, c0 + 64);
+    const int c0 = blockIdx.x * kBuckets, c1 = min(a.n_buckets, c0 + kBuckets);
     const int parts = p.q_blocks * p.b_chunks;
     const float *w = a.ws + static_cast<int64_t>(h) * parts * p.stride;
-    const int step_q = p.b_chunks ? 16 / p.b_chunks : 0, step_b = p.b_chunks ? 16 % p.b_chunks : 0;
+    const int k0 = wave * 4 + (lane >> 4);                 // the quarter's first vector
+    const int step_q = p.b_chunks ? 64 / p.b_chunks : 0, step_b = p.b_chunks ? 64 % p.b_chunks : 0;
+    const int start_q = p.b_chunks ? k0 / p.b_chunks : 0, start_b = k0 - start_q * p.b_chunks;
     float acc = 0.0f;                                     // of bucket c0 + lane, in wavefront 0
     for (int r0 = 0; r0 < n_rel; r0 += 1024) {
         const int c = r0 + tid < n_rel ? a.of[r0 + tid] : -1;
@@ -856,30 +878,34 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
             of[at] = c - c0;
         }
         __syncthreads();
-        for (int e0 = 0; e0 < all; e0 += 64) {
-            const int r = e0 + lane < all ? list[e0 + lane] : -1;
+        for (int e0 = 0; e0 < all; e0 += 16) {
+            const int e = e0 + (lane & 15), r = e < all ? list[e] : -1;
             float t = 0.0f;
-            int qb = wave / p.b_chunks, bc = wave - qb * p.b_chunks;              // the same for the wavefront, as what follows from them
-            for (int k = wave; k < parts; k += 16 * 12) {
-                float v[12];
+            int qb = start_q, bc = start_b;
+            for (int k = k0; k < parts; k += 64 * 4) {
+                float v[4];
 #pragma unroll
-                for (int i = 0; i < 12; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     const int q0 = qb * p.q_block, q1 = min(a.Q, q0 + p.q_block);
                     const int lo = p.map.first(q1), hi = p.map.last(q0);
                     v[i] = 0.0f;
-                    if (k + 16 * i < parts && r >= lo && r <= hi) v[i] = w[static_cast<int64_t>(k + 16 * i) * p.stride + r - lo];
+                    if (k + 64 * i < parts && r >= lo && r <= hi) v[i] = w[static_cast<int64_t>(k + 64 * i) * p.stride + r - lo];
                     qb += step_q, bc += step_b;
                     if (bc >= p.b_chunks) bc -= p.b_chunks, ++qb;
                 }
 #pragma unroll
-                for (int i = 0; i < 12; ++i) t += v[i];
+                for (int i = 0; i < 4; ++i) t += v[i];
             }
-            part[wave][lane] = t;
+            float lo, hi;                                 // the quarters' sums
+            lane_pair<16>(t, &lo, &hi), t = lo + hi;
+            lane_pair<32>(t, &lo, &hi), t = lo + hi;
+            if (lane < 16) part[wave][lane] = t;
             __syncthreads();
             if (wave == 0) {
-                t = part[0][lane];
-                for (int i = 1; i < 16; ++i) t += part[i][lane];
-                bucket_add(r >= 0 ? of[e0 + lane] : -1, t, acc, owner);
+                t = 0.0f;
+                if (lane < 16)
+                    for (int i = 0; i < 16; ++i) t += part[i][lane];
+                bucket_add(lane < 16 && r >= 0 ? of[e] : -1, t, acc, owner);
             }
             __syncthreads();
         }
@@ -913,17 +939,22 @@ template <typename T, bool BACK>
 static hipError_t by_length(const RelArgs &a, const RelPlan &p, hipStream_t st)
 {
     const bool grid = p.map.w != 0;
+    if (p.batch) {
+        switch (p.lanes * 16 + p.nv) {
+            case 8 * 16 + 1: return run(k_rel_rows<T, 8, 1, BACK>, a, p, BACK, st);
+            case 16 * 16 + 1: return run(k_rel_rows<T, 16, 1, BACK>, a, p, BACK, st);
+            case 32 * 16 + 1: return run(k_rel_rows<T, 32, 1, BACK>, a, p, BACK, st);
+            case 32 * 16 + 2: return run(k_rel_rows<T, 32, 2, BACK>, a, p, BACK, st);
+            default: return run(k_rel_rows<T, 64, 2, BACK>, a, p, BACK, st);
+        }
+    }
     switch (p.lanes * 16 + p.nv) {
-        case 8 * 16 + 1: return run(k_rel_rows<T, 8, BACK>, a, p, BACK, st);
-        case 16 * 16 + 1: return run(k_rel_rows<T, 16, BACK>, a, p, BACK, st);
-        case 32 * 16 + 1: return run(k_rel_rows<T, 32, BACK>, a, p, BACK, st);
-        case 64 * 16 + 1: return run(grid ? k_rel_long<T, 64, 1, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 64, 1, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
-        case 64 * 16 + 2: return run(grid ? k_rel_long<T, 64, 2, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 64, 2, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
-        case 64 * 16 + 4: return run(grid ? k_rel_long<T, 64, 4, true, BACK, LONG_AHEAD, LONG_WAVES> : k_rel_long<T, 64, 4, false, BACK, LONG_AHEAD, LONG_WAVES>, a, p, BACK, st);
-        case 256 * 16 + 1: return run(grid ? k_rel_long<T, 256, 1, true, BACK, LONG_AHEAD, 1> : k_rel_long<T, 256, 1, false, BACK, LONG_AHEAD, 1>, a, p, BACK, st);
-        case 256 * 16 + 2: return run(grid ? k_rel_long<T, 256, 2, true, BACK, false, 1> : k_rel_long<T, 256, 2, false, BACK, false, 1>, a, p, BACK, st);
-        case 256 * 16 + 4: return run(k_rel_long<T, 256, 4, false, BACK, false, 1>, a, p, BACK, st);
-        default: return run(k_rel_long<T, 256, 8, false, BACK, false, 1>, a, p, BACK, st);
+        case 64 * 16 + 1: return run(grid ? k_rel_long<T, 64, 1, true, BACK> : k_rel_long<T, 64, 1, false, BACK>, a, p, BACK, st);
+        case 64 * 16 + 2: return run(grid ? k_rel_long<T, 64, 2, true, BACK> : k_rel_long<T, 64, 2, false, BACK>, a, p, BACK, st);
+        case 64 * 16 + 4: return run(grid ? k_rel_long<T, 64, 4, true, BACK> : k_rel_long<T, 64, 4, false, BACK>, a, p, BACK, st);
+        case 256 * 16 + 2: return run(grid ? k_rel_long<T, 256, 2, true, BACK> : k_rel_long<T, 256, 2, false, BACK>, a, p, BACK, st);
+        case 256 * 16 + 4: return run(k_rel_long<T, 256, 4, false, BACK>, a, p, BACK, st);
+        default: return run(k_rel_long<T, 256, 8, false, BACK>, a, p, BACK, st);
     }
 }
 
@@ -944,7 +975,7 @@ hipError_t launch_rel_softmax_backward(const RelArgs &a, hipStream_t st)
     }
     if (!a.dtable) return hipSuccess;
     if (p.few) k_rel_few_buckets<<<a.H, 1024, 0, st>>>(a, p);
-    else k_rel_many_buckets<<<dim3((a.n_buckets + 63) / 64, a.H), 1024, 0, st>>>(a, p, n_rel);      // without rows: zeros
+    else k_rel_many_buckets<<<dim3((a.n_buckets + kBuckets - 1) / kBuckets, a.H), 1024, 0, st>>>(a, p, n_rel);      // without rows: zeros
     return hipGetLastError();
 }
 
