@@ -846,29 +846,30 @@ __global__ __launch_bounds__(1024) void k_rel_few_buckets(RelArgs a, RelPlan p)
 }
 
 // The same for many buckets, 16 of them from 16 * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
-// belong to the 16 buckets are listed in their order, 1024 at a time; 16 of the list go through the workgroups' vectors together, a quarter
-// of a wavefront to every 64th vector, and then to their buckets, a lane each.
-constexpr int kBuckets = 16;
-__global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel)
+// belong to the 16 buckets are listed in their order, 512 at a time; 16 of the list go through the workgroups' vectors together, a quarter
+// of a wavefront to every 32nd vector, and then to their buckets, a lane each.
+constexpr int kBuckets = 16, kManyThreads = 512, kQuarters = kManyThreads / 16;
+__global__ __launch_bounds__(kManyThreads) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel)
 {
-    __shared__ int list[1024], of[1024], count[16], owner[64];
-    __shared__ float part[16][kBuckets];
+    constexpr int WAVES = kManyThreads / 64;
+    __shared__ int list[kManyThreads], of[kManyThreads], count[WAVES], owner[64];
+    __shared__ float part[WAVES][kBuckets];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = blockIdx.y;
     const int c0 = blockIdx.x * kBuckets, c1 = min(a.n_buckets, c0 + kBuckets);
     const int parts = p.q_blocks * p.b_chunks;
     const float *w = a.ws + static_cast<int64_t>(h) * parts * p.stride;
     const int k0 = wave * 4 + (lane >> 4);                 // the quarter's first vector
-    const int step_q = p.b_chunks ? 64 / p.b_chunks : 0, step_b = p.b_chunks ? 64 % p.b_chunks : 0;
+    const int step_q = p.b_chunks ? kQuarters / p.b_chunks : 0, step_b = p.b_chunks ? kQuarters % p.b_chunks : 0;
     const int start_q = p.b_chunks ? k0 / p.b_chunks : 0, start_b = k0 - start_q * p.b_chunks;
     float acc = 0.0f;                                     // of bucket c0 + lane, in wavefront 0
-    for (int r0 = 0; r0 < n_rel; r0 += 1024) {
+    for (int r0 = 0; r0 < n_rel; r0 += kManyThreads) {
         const int c = r0 + tid < n_rel ? a.of[r0 + tid] : -1;
         const bool in = c >= c0 && c < c1;
         const uint64_t ballot = __ballot(in);
         if (lane == 0) count[wave] = __popcll(ballot);
         __syncthreads();
         int before = 0, all = 0;
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             before += i < wave ? count[i] : 0;
             all += count[i];
         }
@@ -882,19 +883,19 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
             const int e = e0 + (lane & 15), r = e < all ? list[e] : -1;
             float t = 0.0f;
             int qb = start_q, bc = start_b;
-            for (int k = k0; k < parts; k += 64 * 4) {
-                float v[4];
+            for (int k = k0; k < parts; k += kQuarters * 8) {
+                float v[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     const int q0 = qb * p.q_block, q1 = min(a.Q, q0 + p.q_block);
                     const int lo = p.map.first(q1), hi = p.map.last(q0);
                     v[i] = 0.0f;
-                    if (k + 64 * i < parts && r >= lo && r <= hi) v[i] = w[static_cast<int64_t>(k + 64 * i) * p.stride + r - lo];
+                    if (k + kQuarters * i < parts && r >= lo && r <= hi) v[i] = w[static_cast<int64_t>(k + kQuarters * i) * p.stride + r - lo];
                     qb += step_q, bc += step_b;
                     if (bc >= p.b_chunks) bc -= p.b_chunks, ++qb;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t += v[i];
+                for (int i = 0; i < 8; ++i) t += v[i];
             }
             float lo, hi;                                 // the quarters' sums
             lane_pair<16>(t, &lo, &hi), t = lo + hi;
@@ -904,7 +905,7 @@ __global__ __launch_bounds__(1024) void k_rel_many_buckets(RelArgs a, RelPlan p,
             if (wave == 0) {
                 t = 0.0f;
                 if (lane < 16)
-                    for (int i = 0; i < 16; ++i) t += part[i][lane];
+                    for (int i = 0; i < WAVES; ++i) t += part[i][lane];
                 bucket_add(lane < 16 && r >= 0 ? of[e] : -1, t, acc, owner);
             }
             __syncthreads();
@@ -975,7 +976,7 @@ hipError_t launch_rel_softmax_backward(const RelArgs &a, hipStream_t st)
     }
     if (!a.dtable) return hipSuccess;
     if (p.few) k_rel_few_buckets<<<a.H, 1024, 0, st>>>(a, p);
-    else k_rel_many_buckets<<<dim3((a.n_buckets + kBuckets - 1) / kBuckets, a.H), 1024, 0, st>>>(a, p, n_rel);      // without rows: zeros
+    else k_rel_many_buckets<<<dim3((a.n_buckets + kBuckets - 1) / kBuckets, a.H), kManyThreads, 0, st>>>(a, p, n_rel);      // without rows: zeros
     return hipGetLastError();
 }
 
