@@ -1,0 +1,118 @@
+"""Residual blocks of a hybrid image network (convolution stages, then attention stages, as EfficientFormer has them) whose layers train
+with HLQ and whose normalisation, activation, dropout and attention maps are this library's kernels as well.
+
+``python -m paper_2406_15102_amd.blocks`` trains a small one on synthetic images and prints the loss.  torch multiplies queries with
+keys and the map with the values; everything between those products and the layers' is one launch each way or two.
+"""
+from __future__ import annotations
+
+import argparse
+
+import torch
+
+from .autograd import HlqConv2d, HlqDropout, HlqGroupNormAct, HlqLinear, HlqRelSoftmax
+
+
+class _BatchedProduct(torch.autograd.Function):
+    """a [G, M, K] times b [G, K, N]; every operand is dense before it is multiplied, in the backward pass too."""
+
+    @staticmethod
+    def forward(ctx, a, b):
+        a, b = a.contiguous(), b.contiguous()
+        ctx.save_for_backward(a, b)
+        return torch.bmm(a, b)
+
+    @staticmethod
+    def backward(ctx, g):
+        a, b = ctx.saved_tensors
+        g = g.contiguous()
+        return torch.bmm(g, b.transpose(1, 2).contiguous()), torch.bmm(a.transpose(1, 2).contiguous(), g)
+
+
+class HlqConvBlock(torch.nn.Module):
+    """x + conv(dropout(silu(norm(conv(silu(norm(x))))))) on channels-last images [Nb, C, H, W]."""
+
+    def __init__(self, channels, groups=8, p=0.0, device="cuda", seed=0, **hlq):
+        super().__init__()
+        self.norm1 = HlqGroupNormAct(groups, channels, act="silu", device=device, seed=seed)
+        self.conv1 = HlqConv2d(channels, channels, 3, padding=1, device=device, seed=seed, **hlq)
+        self.norm2 = HlqGroupNormAct(groups, channels, act="silu", p=p, device=device, seed=seed)
+        self.conv2 = HlqConv2d(channels, channels, 3, padding=1, device=device, seed=seed, **hlq)
+
+    def forward(self, x):
+        return x + self.conv2(self.norm2(self.conv1(self.norm1(x))))
+
+
+class HlqAttentionBlock(torch.nn.Module):
+    """x + dropout(proj(map values)) over the positions of channels-last images [Nb, C, H, W], the map with a learned bias for every
+    head and relative position; the tokens of all images together are a multiple of 16."""
+
+    def __init__(self, channels, heads, grid, groups=1, p=0.0, p_map=0.0, device="cuda", seed=0, **hlq):
+        super().__init__()
+        if channels % heads:
+            raise ValueError("%d channels are no whole heads of %d" % (channels, heads))
+        self.heads, self.grid = heads, tuple(grid)
+        self.norm = HlqGroupNormAct(groups, channels, device=device, seed=seed)
+        self.qkv = HlqLinear(channels, 3 * channels, device=device, seed=seed, **hlq)
+        self.map = HlqRelSoftmax(heads, grid=self.grid, scale=(channels // heads) ** -0.5, p=p_map, device=device, seed=seed)
+        self.proj = HlqLinear(channels, channels, device=device, seed=seed, **hlq)
+        self.drop = HlqDropout(p, seed=seed)
+
+    def forward(self, x):
+        Nb, C, H, W = x.shape
+        if (H, W) != self.grid:
+            raise ValueError("image of %dx%d positions, the block's grid is %dx%d" % (H, W, *self.grid))
+        n, h, d = H * W, self.heads, C // self.heads
+        tokens = x.permute(0, 2, 3, 1).reshape(Nb, n, C)                                 # a view
+        y = self.norm(x).permute(0, 2, 3, 1).reshape(Nb * n, C)
+        q, k, v = self.qkv(y).reshape(Nb, n, 3, h, d).permute(2, 0, 3, 1, 4).reshape(3, Nb * h, n, d).unbind(0)
+        scores = _BatchedProduct.apply(q, k.transpose(1, 2)).reshape(Nb, h, n, n)
+        out = _BatchedProduct.apply(self.map(scores).reshape(Nb * h, n, n), v)
+        out = self.proj(out.reshape(Nb, h, n, d).permute(0, 2, 1, 3).reshape(Nb * n, C))
+        return self.drop(out.reshape(Nb, n, C), tokens).reshape(Nb, H, W, C).permute(0, 3, 1, 2)
+
+
+class HybridNet(torch.nn.Module):
+    """A convolution stage, a strided convolution, an attention stage and a classifier on images [Nb, c_in, 2 g, 2 g]."""
+
+    def __init__(self, c_in=16, width=64, grid=8, heads=4, classes=10, p=0.1, device="cuda", seed=0):
+        super().__init__()
+        self.stem = HlqConv2d(c_in, width, 3, padding=1, device=device, seed=seed)
+        self.conv = HlqConvBlock(width, p=p, device=device, seed=seed)
+        self.down = HlqConv2d(width, 2 * width, 3, stride=2, padding=1, device=device, seed=seed)
+        self.attend = HlqAttentionBlock(2 * width, heads, (grid, grid), groups=8, p=p, p_map=p, device=device, seed=seed)
+        self.norm = HlqGroupNormAct(8, 2 * width, act="gelu", device=device, seed=seed)
+        self.head = torch.nn.Linear(2 * width, classes, device=device, dtype=torch.float32)
+
+    def forward(self, x):
+        y = self.norm(self.attend(self.down(self.conv(self.stem(x)))))
+        return self.head(y.float().mean((2, 3)))
+
+
+def train(steps=20, batch=16, grid=8, classes=10, lr=2e-3, device="cuda", seed=0):
+    """Losses of a few steps on synthetic images: a class's images share a pattern under noise."""
+    g = torch.Generator(device=device).manual_seed(seed)
+    torch.manual_seed(seed)
+    net = HybridNet(grid=grid, classes=classes, device=device, seed=seed)
+    opt = torch.optim.AdamW(net.parameters(), lr=lr)
+    patterns = torch.randn((classes, 16, 2 * grid, 2 * grid), generator=g, device=device)
+    losses = []
+    for _ in range(steps):
+        label = torch.randint(0, classes, (batch,), generator=g, device=device)
+        x = patterns[label] + 0.5 * torch.randn((batch, 16, 2 * grid, 2 * grid), generator=g, device=device)
+        x = x.bfloat16().contiguous(memory_format=torch.channels_last)
+        loss = torch.nn.functional.cross_entropy(net(x), label)
+        opt.zero_grad(set_to_none=True)
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+    return [float(v) for v in losses]
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--steps", type=int, default=40)
+    ap.add_argument("--batch", type=int, default=16)
+    a = ap.parse_args()
+    for i, v in enumerate(train(a.steps, a.batch)):
+        print("step %3d  loss %.4f" % (i, v))
