@@ -13,6 +13,7 @@ namespace hlq {
 typedef uint32_t raw4_t __attribute__((ext_vector_type(4)));
 typedef raw4_t raw4_e2 __attribute__((aligned(2)));
 typedef uint32_t raw2_t __attribute__((ext_vector_type(2)));
+typedef raw2_t raw2_e2 __attribute__((aligned(2)));
 typedef uint32_t raw1_e2 __attribute__((aligned(2)));
 typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef f4_t f4_e4 __attribute__((aligned(4)));
@@ -60,6 +61,20 @@ template <> struct Raw<float, 8> {
         *reinterpret_cast<f4_e4 *>(p + 4) = b;
     }
 };
+template <> struct Raw<bf16_t, 4> {
+    raw2_t w;
+    __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const raw2_e2 *>(p); }
+    __device__ __forceinline__ void zero() { w = raw2_t{0u, 0u}; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = bf16_lo(w[0]), v[1] = bf16_hi(w[0]), v[2] = bf16_lo(w[1]), v[3] = bf16_hi(w[1]); }
+    __device__ __forceinline__ void pack(const float *v) { w = raw2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
+};
+template <> struct Raw<float, 4> {
+    f4_t w;
+    __device__ __forceinline__ void load(const float *p) { w = *reinterpret_cast<const f4_e4 *>(p); }
+    __device__ __forceinline__ void zero() { w = f4_t{0.0f, 0.0f, 0.0f, 0.0f}; }
+    __device__ __forceinline__ void widen(float *v) const { v[0] = w[0], v[1] = w[1], v[2] = w[2], v[3] = w[3]; }
+    __device__ __forceinline__ void pack(const float *v) { w = f4_t{v[0], v[1], v[2], v[3]}; }
+};
 template <> struct Raw<bf16_t, 2> {
     uint32_t w;
     __device__ __forceinline__ void load(const bf16_t *p) { w = *reinterpret_cast<const raw1_e2 *>(p); }
@@ -105,6 +120,8 @@ __device__ __forceinline__ void buffer_load(Raw<float, 8> &r, __amdgpu_buffer_rs
     r.a = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
     r.b = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at + 16, 0, 0));
 }
+__device__ __forceinline__ void buffer_load(Raw<bf16_t, 4> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b64(b, at, 0, 0); }
+__device__ __forceinline__ void buffer_load(Raw<float, 4> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_bit_cast(f4_t, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0)); }
 __device__ __forceinline__ void buffer_load(Raw<bf16_t, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0); }
 __device__ __forceinline__ void buffer_load(Raw<float, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_bit_cast(f2_t, __builtin_amdgcn_raw_buffer_load_b64(b, at, 0, 0)); }
 __device__ __forceinline__ void buffer_load(Raw<bf16_t, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { r.w = __builtin_amdgcn_raw_buffer_load_b16(b, at, 0, 0); }
@@ -116,6 +133,8 @@ __device__ __forceinline__ void buffer_store(const Raw<float, 8> &r, __amdgpu_bu
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw4_t, r.a), b, at, 0, 0);
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw4_t, r.b), b, at + 16, 0, 0);
 }
+__device__ __forceinline__ void buffer_store(const Raw<bf16_t, 4> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b64(r.w, b, at, 0, 0); }
+__device__ __forceinline__ void buffer_store(const Raw<float, 4> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw4_t, r.w), b, at, 0, 0); }
 __device__ __forceinline__ void buffer_store(const Raw<bf16_t, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b32(r.w, b, at, 0, 0); }
 __device__ __forceinline__ void buffer_store(const Raw<float, 2> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(raw2_t, r.w), b, at, 0, 0); }
 __device__ __forceinline__ void buffer_store(const Raw<bf16_t, 1> &r, __amdgpu_buffer_rsrc_t b, uint32_t at) { __builtin_amdgcn_raw_buffer_store_b16(r.w, b, at, 0, 0); }
@@ -268,7 +287,22 @@ __device__ __forceinline__ void drop_raw(Raw<float, 8> &r, uint32_t word, const 
         }
     }
 }
-// the same for vectors of 2 and 1, `i` the first element
+// the same for vectors of 4, 2 and 1, `i` the first element, a multiple of their number
+template <typename T> __device__ __forceinline__ void drop_raw(Raw<T, 4> &r, int64_t i, const DropRule &d)
+{
+    uint32_t w[2];
+    rand_words<2>(static_cast<uint32_t>(i >> 1), d.k0, d.k1, w);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const bool lo = (w[k] & 0xFFFFu) >= d.below, hi = (w[k] >> 16) >= d.below;
+        if constexpr (sizeof(T) == 2) {
+            r.w[k] &= (lo ? 0xFFFFu : 0u) | (hi ? 0xFFFF0000u : 0u);
+        } else {
+            r.w[2 * k] = lo ? r.w[2 * k] : 0.0f;
+            r.w[2 * k + 1] = hi ? r.w[2 * k + 1] : 0.0f;
+        }
+    }
+}
 template <typename T> __device__ __forceinline__ void drop_raw(Raw<T, 2> &r, int64_t i, const DropRule &d)
 {
     uint32_t w;

@@ -33,7 +33,7 @@ int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 // widest vector that channels allow, and the smallest slab of whole groups and whole vectors
 bool slab_unit(int C, int cg, int *ve, int *unit)
 {
-    for (int v : {8, 2, 1}) {
+    for (int v : {8, 4, 2, 1}) {
         if (C % v) continue;
         const int64_t u = static_cast<int64_t>(cg) / gcd(cg, v) * v;
         if (u <= kMaxSlab && u / v <= 1024) {
@@ -879,6 +879,7 @@ static hipError_t by_vector(const GroupNormArgs &a, bool back, hipStream_t st)
 {
     const GroupNormPlan p = plan_for(a.Nb, a.P, a.C, a.cg, a.is_f32, back);
     if (p.ve == 8) return by_threads<T, 8>(a, p, back, st);
+    if (p.ve == 4) return by_threads<T, 4>(a, p, back, st);
     if (p.ve == 2) return by_threads<T, 2>(a, p, back, st);
     return by_threads<T, 1>(a, p, back, st);
 }

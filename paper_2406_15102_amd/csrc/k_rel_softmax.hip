@@ -107,7 +107,7 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     const int resident = rel_resident(p, back);
     int chunks = 1, q_per = 1;
     int64_t best = INT64_MAX;
-    for (int m = 1; m <= resident; ++m) {
+    for (int m = 1; m <= 2 * resident; ++m) {
         const int64_t target = 256 * m;
         const int n = static_cast<int>(std::min<int64_t>(b_steps, std::max<int64_t>(1, target / lines)));
         const int per = static_cast<int>(std::min<int64_t>(q_steps, std::max<int64_t>(1, (lines + target - 1) / target)));
