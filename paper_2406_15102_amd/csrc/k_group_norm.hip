@@ -759,12 +759,12 @@ __global__ __launch_bounds__(THREADS) void k_gn_grad_apply(GroupNormArgs a, Grou
         const int seg = i / s.ncol, col = i - seg * s.ncol;
         float A = 0.0f, B = 0.0f;
         if (s.c0 + col < a.C) {
-            for (int k = seg; k < p.chunks; k += 4 * segs) {
-                float2 v[4];
+            for (int k = seg; k < p.chunks; k += 8 * segs) {
+                float2 v[8];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = k + u * segs < p.chunks ? part[static_cast<int64_t>(k + u * segs) * a.C + col] : make_float2(0.0f, 0.0f);
+                for (int u = 0; u < 8; ++u) v[u] = k + u * segs < p.chunks ? part[static_cast<int64_t>(k + u * segs) * a.C + col] : make_float2(0.0f, 0.0f);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) A += v[u].x, B += v[u].y;
+                for (int u = 0; u < 8; ++u) A += v[u].x, B += v[u].y;
             }
         }
         pA[i] = A, pB[i] = B;

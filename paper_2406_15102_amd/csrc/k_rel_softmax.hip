@@ -820,42 +820,44 @@ __global__ __launch_bounds__(kThreads, NV >= 8 ? 1 : 2) void k_rel_long(RelArgs 
     }
 }
 
-// dtable[c, h] of head blockIdx.x where the workgroups have summed by bucket: 16 wavefronts take their rows in turns, a lane a bucket.
+// dtable[c, h] of head blockIdx.x, 16 buckets from 16 * blockIdx.y on, where the workgroups have summed by bucket: 64 quarters of a wavefront take
+// the workgroups' sums in turns, a lane a bucket.
 __global__ __launch_bounds__(1024) void k_rel_few_buckets(RelArgs a, RelPlan p)
 {
-    __shared__ float part[16][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = blockIdx.x, parts = p.q_blocks * p.b_chunks;
-    const float *w = a.ws + static_cast<int64_t>(h) * parts * kFewBuckets + lane;
+    __shared__ float part[16][16];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = blockIdx.x, parts = p.q_blocks * p.b_chunks, c = blockIdx.y * 16 + (lane & 15);
+    const float *w = a.ws + static_cast<int64_t>(h) * parts * kFewBuckets + c;
     float t = 0.0f;
-    int k = wave;
-    for (; k + 7 * 16 < parts; k += 8 * 16) {
+    for (int k = wave * 4 + (lane >> 4); k < parts; k += 64 * 8) {
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = w[(k + 16 * i) * kFewBuckets];
+        for (int i = 0; i < 8; ++i) v[i] = k + 64 * i < parts ? w[static_cast<int64_t>(k + 64 * i) * kFewBuckets] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) t += v[i];
     }
-    for (; k < parts; k += 16) t += w[k * kFewBuckets];
-    part[wave][lane] = t;
+    float lo, hi;                                         // the quarters' sums
+    lane_pair<16>(t, &lo, &hi), t = lo + hi;
+    lane_pair<32>(t, &lo, &hi), t = lo + hi;
+    if (lane < 16) part[wave][lane] = t;
     __syncthreads();
-    if (wave == 0 && lane < a.n_buckets) {
+    if (wave == 0 && lane < 16 && c < a.n_buckets) {
         t = part[0][lane];
         for (int i = 1; i < 16; ++i) t += part[i][lane];
-        store_param(a.dtable, a.param_f32, static_cast<int64_t>(lane) * a.H + h, t);
+        store_param(a.dtable, a.param_f32, static_cast<int64_t>(c) * a.H + h, t);
     }
 }
 
-// The same for many buckets, 16 of them from 16 * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
-// belong to the 16 buckets are listed in their order, 512 at a time; 16 of the list go through the workgroups' vectors together, a quarter
+// The same for many buckets, `per` of them, at most 16, from per * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
+// belong to the buckets are listed in their order, 512 at a time; 16 of the list go through the workgroups' vectors together, a quarter
 // of a wavefront to every 32nd vector, and then to their buckets, a lane each.
 constexpr int kBuckets = 16, kManyThreads = 512, kQuarters = kManyThreads / 16;
-__global__ __launch_bounds__(kManyThreads) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel)
+__global__ __launch_bounds__(kManyThreads) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel, int per)
 {
     constexpr int WAVES = kManyThreads / 64;
     __shared__ int list[kManyThreads], of[kManyThreads], count[WAVES], owner[64];
     __shared__ float part[WAVES][kBuckets];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = blockIdx.y;
-    const int c0 = blockIdx.x * kBuckets, c1 = min(a.n_buckets, c0 + kBuckets);
+    const int c0 = blockIdx.x * per, c1 = min(a.n_buckets, c0 + per);
     const int parts = p.q_blocks * p.b_chunks;
     const float *w = a.ws + static_cast<int64_t>(h) * parts * p.stride;
     const int k0 = wave * 4 + (lane >> 4);                 // the quarter's first vector
@@ -927,7 +929,7 @@ static hipError_t run(void (*f)(RelArgs, RelPlan), const RelArgs &a, const RelPl
 {
     const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.H) * p.q_blocks * p.b_chunks);
     const size_t lds = rel_lds_bytes(p, back);
-    if (lds > 65536)
+    if (lds + 4096 > 65536)                               // with what the kernels declare themselves, less than 4 KB
         if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds))) {
             (void)hipGetLastError();
             return e;
@@ -975,8 +977,14 @@ hipError_t launch_rel_softmax_backward(const RelArgs &a, hipStream_t st)
         if (const hipError_t e = a.is_f32 ? by_length<float, true>(a, p, st) : by_length<bf16_t, true>(a, p, st)) return e;
     }
     if (!a.dtable) return hipSuccess;
-    if (p.few) k_rel_few_buckets<<<a.H, 1024, 0, st>>>(a, p);
-    else k_rel_many_buckets<<<dim3((a.n_buckets + kBuckets - 1) / kBuckets, a.H), kManyThreads, 0, st>>>(a, p, n_rel);      // without rows: zeros
+    if (p.few) k_rel_few_buckets<<<dim3(a.H, (a.n_buckets + 15) / 16), 1024, 0, st>>>(a, p);
+    else {
+        // Fewer buckets a workgroup where units would idle and the lists are long: 3 heads' 144 distances of a 12 x 12 grid took 22.9 us with 16
+        // and 16.3 us with one. With short lists (a bucket an offset) the scan for them is the cost, and 16 stay: 15.2 against 18.1 us.
+        int per = kBuckets;
+        while (per > 1 && per * static_cast<int64_t>(n_rel) > 16 * a.n_buckets && static_cast<int64_t>((a.n_buckets + per - 1) / per) * a.H < 256) per /= 2;
+        k_rel_many_buckets<<<dim3((a.n_buckets + per - 1) / per, a.H), kManyThreads, 0, st>>>(a, p, n_rel, per);      // without rows: zeros
+    }
     return hipGetLastError();
 }
 
