@@ -174,8 +174,8 @@ __device__ __forceinline__ void load_inside(Raw<T, 8> &r, const T *base, int64_t
         for (int e = 0; e < 8; ++e) push_element(r, at + e < total ? base[at + e] : T{});
     }
 }
-// bit e: byte e of the eight is not zero
-__device__ __forceinline__ uint32_t load_mask(const uint8_t *base, int64_t at, int64_t total)
+// eight of the mask's bytes, zeros beyond its end; what is made of them waits for them, so it is left to the place that needs it
+__device__ __forceinline__ uint64_t load_mask(const uint8_t *base, int64_t at, int64_t total)
 {
     uint64_t m = 0;
     if (at + 8 <= total) {
@@ -184,9 +184,14 @@ __device__ __forceinline__ uint32_t load_mask(const uint8_t *base, int64_t at, i
 #pragma unroll 1
         for (int e = 0; e < 8 && at + e < total; ++e) m |= static_cast<uint64_t>(base[at + e]) << (8 * e);
     }
-    const uint64_t low = 0x7F7F7F7F7F7F7F7Full;
-    const uint64_t top = (((m & low) + low) | m) & ~low;               // bit 7 of every byte that is not zero
-    return static_cast<uint32_t>((top >> 7) * 0x0102040810204080ull >> 56);
+    return m;
+}
+// bit e: byte e of the eight is not zero
+__device__ __forceinline__ uint32_t mask_bits(uint64_t m)
+{
+    const uint32_t low = 0x7F7F7F7Fu, m0 = static_cast<uint32_t>(m), m1 = static_cast<uint32_t>(m >> 32);
+    const uint32_t t0 = ((((m0 & low) + low) | m0) >> 7) & 0x01010101u, t1 = ((((m1 & low) + low) | m1) >> 7) & 0x01010101u;
+    return __builtin_amdgcn_udot4(t1, 0x80402010u, __builtin_amdgcn_udot4(t0, 0x08040201u, 0u, false), false);      // sums of bytes' products
 }
 // A row's eight to `at` where k0 + 8 <= K; the lane whose eight the row's end cuts stores the K % 8 it has (`cut`: its place, others kNowhere).
 // One store for sure, and others only where K % 8 is not 0: the wait for the loads behind it need not wait for it.
@@ -353,8 +358,8 @@ template <typename T, int NV, bool BACK> struct RelRow {
             const int k0 = first + 8 * lanes * j;
             seen[j] = end - k0 >= 8 ? 0xFFu : end > k0 ? (1u << (end - k0)) - 1u : 0u;
             if (a.mask && k0 < end)
-                seen[j] &= load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0,
-                                     static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K);
+                seen[j] &= mask_bits(load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0,
+                                               static_cast<int64_t>(a.mask_batches) * a.mask_rows * a.K));
         }
     }
 };
@@ -466,9 +471,7 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
     const int64_t reach = (p.rows_b - 1) * plane + (p.rows_q - 1) * a.K + WIDTH;              // the workgroup's end beside its place
     const float keep = a.drop.below ? a.drop.scale : 1.0f;
     Raw<T, 8> ns[NV], nd[NV];
-    uint32_t nbits[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) nbits[j] = 0xFFu;
+    uint64_t nmask[NV];                                       // the mask's bytes
     auto fetch = [&](int qs, int bs) {
         const int q = qs + row_q, b = bs + row_b;
         const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
@@ -489,8 +492,9 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
                 ns[j].zero();
                 if (BACK) nd[j].zero();
             }
+            nmask[j] = 0;
             if (a.mask && k0 < end)
-                nbits[j] = load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0, mask_total);
+                nmask[j] = load_mask(a.mask, (static_cast<int64_t>(b % a.mask_batches) * a.mask_rows + (a.mask_rows > 1 ? q : 0)) * a.K + k0, mask_total);
         }
     };
     fetch(job.q0, job.b0);
@@ -526,9 +530,9 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
         whole = __all(whole);
         for (int bs = job.b0; bs < job.b1; bs += p.rows_b) {
             Raw<T, 8> rs[NV], rd[NV];
-            uint32_t seen[NV];
+            uint64_t mask[NV];
 #pragma unroll
-            for (int j = 0; j < NV; ++j) rs[j] = ns[j], rd[j] = nd[j], seen[j] = nbits[j];
+            for (int j = 0; j < NV; ++j) rs[j] = ns[j], rd[j] = nd[j], mask[j] = nmask[j];
             const bool same = bs + p.rows_b < job.b1;
             fetch(same ? qs : qs + p.rows_q, same ? bs + p.rows_b : job.b0);       // behind the last there is nothing to load
             const int64_t base = (static_cast<int64_t>(bs) * a.H + job.h) * a.Q * a.K + static_cast<int64_t>(qs) * a.K;
@@ -544,9 +548,10 @@ __global__ __launch_bounds__(kThreads) void k_rel_rows(RelArgs a, RelPlan p)
 #pragma unroll
                 for (int e = 8 * j; e < 8 * j + 8; ++e) z[e] = __builtin_fmaf(z[e], a.scale, bv[e]);
                 if (a.mask) {
+                    const uint32_t seen = mask_bits(mask[j]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[8 * j + e] = (seen[j] >> e) & 1u ? z[8 * j + e] : NONE;
-                    if (BACK) keep_bits(rd[j], seen[j]);               // whatever stands where nothing is seen
+                    for (int e = 0; e < 8; ++e) z[8 * j + e] = (seen >> e) & 1u ? z[8 * j + e] : NONE;
+                    if (BACK) keep_bits(rd[j], seen);                  // whatever stands where nothing is seen
                 }
             }
 #pragma unroll

@@ -128,6 +128,24 @@ def test_masks_that_leave_rows_empty(Q, K, grid_w, rows, dtype):
             _check(s, dP, *args, out)
 
 
+@pytest.mark.parametrize("B", [1, 3, 5])
+@pytest.mark.parametrize("Q,K", [(1, 5), (3, 40), (3, 130), (5, 300), (3, 700), (2, 3000)])
+def test_table_values_that_nothing_sees(B, Q, K):
+    """A value of the table that only masked places reach changes nothing, whatever it is, and its gradient is zero."""
+    s, dP, table, of = _inputs(B, 2, Q, K, 0, F32, F32)
+    of[Q] = 3
+    of[np.arange(len(of)) != Q] %= 3
+    mask = torch.from_numpy(_rel_index(Q, K, 0) != Q).to(torch.uint8)[None] * 255
+    want = _call(s, dP, table, of, mask, 0, False, 0.5, 0.1, 3)
+    _check(s, dP, table, of, mask, 0, False, 0.5, 0.1, 3, want)
+    for junk in (float("nan"), float("inf"), -float("inf"), torch.finfo(F32).min):
+        other = table.clone()
+        other[3] = junk
+        got = _call(s, dP, other, of, mask, 0, False, 0.5, 0.1, 3)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        assert not bool(got[2][3].any())
+
+
 def test_scores_of_minus_infinity_and_the_lowest_value():
     for dtype in (BF16, F32):
         s, dP, table, of = _inputs(2, 2, 6, 70, 0, dtype, F32)
