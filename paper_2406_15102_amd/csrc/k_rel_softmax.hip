@@ -83,11 +83,14 @@ RelPlan rel_plan(const RelArgs &a, bool back)
     p.map = rel_map(a);
     const int gw = p.map.w;
     // Rows through the batch (k_rel_rows) up to 1024 keys where there is a batch to go through, else a row at a time.
+    // 513 to 768 keys in 32 lanes leave fewer lanes idle than in 64 but take more registers: 16 x 8 maps of 576 x 576 take 52.9 us forward on bf16
+    // where 64 lanes take 59.4, but 94.5 against 92.7 backward, and on fp32 87.8 against 84.3 and 142 against 128.
     p.batch = a.K <= 256 || (a.K <= 1024 && a.B >= 4);
     if (a.K <= 64) p.lanes = 8, p.nv = 1;
     else if (a.K <= 128) p.lanes = 16, p.nv = 1;
     else if (a.K <= 256) p.lanes = 32, p.nv = 1;
     else if (a.K <= 512) p.lanes = p.batch ? 32 : 64, p.nv = p.batch ? 2 : 1;
+    else if (a.K <= 768 && p.batch && !back && !a.is_f32) p.lanes = 32, p.nv = 3;
     else if (a.K <= 1024) p.lanes = 64, p.nv = 2;
     else if (a.K <= 2048) p.lanes = 64, p.nv = 4;
     else if (a.K <= 4096) p.lanes = 256, p.nv = 2;
@@ -853,13 +856,14 @@ __global__ __launch_bounds__(1024) void k_rel_few_buckets(RelArgs a, RelPlan p)
 }
 
 // The same for many buckets, `per` of them, at most 16, from per * blockIdx.x on of head blockIdx.y, from the workgroups' sums by relative position: those that
-// belong to the buckets are listed in their order, 512 at a time; 16 of the list go through the workgroups' vectors together, a quarter
+// belong to the buckets are listed in their order, 1024 at a time; 16 of the list go through the workgroups' vectors together, a quarter
 // of a wavefront to every 32nd vector, and then to their buckets, a lane each.
-constexpr int kBuckets = 16, kManyThreads = 512, kQuarters = kManyThreads / 16;
+constexpr int kBuckets = 16, kManyThreads = 512, kQuarters = kManyThreads / 16, kScan = 2;
 __global__ __launch_bounds__(kManyThreads) void k_rel_many_buckets(RelArgs a, RelPlan p, int n_rel, int per)
 {
     constexpr int WAVES = kManyThreads / 64;
-    __shared__ int list[kManyThreads], of[kManyThreads], count[WAVES], owner[64];
+    __shared__ int list[kScan * kManyThreads], count[kScan * WAVES], owner[64];
+    __shared__ uint8_t of[kScan * kManyThreads];
     __shared__ float part[WAVES][kBuckets];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, h = blockIdx.y;
     const int c0 = blockIdx.x * per, c1 = min(a.n_buckets, c0 + per);
@@ -869,21 +873,34 @@ __global__ __launch_bounds__(kManyThreads) void k_rel_many_buckets(RelArgs a, Re
     const int step_q = p.b_chunks ? kQuarters / p.b_chunks : 0, step_b = p.b_chunks ? kQuarters % p.b_chunks : 0;
     const int start_q = p.b_chunks ? k0 / p.b_chunks : 0, start_b = k0 - start_q * p.b_chunks;
     float acc = 0.0f;                                     // of bucket c0 + lane, in wavefront 0
-    for (int r0 = 0; r0 < n_rel; r0 += kManyThreads) {
-        const int c = r0 + tid < n_rel ? a.of[r0 + tid] : -1;
-        const bool in = c >= c0 && c < c1;
-        const uint64_t ballot = __ballot(in);
-        if (lane == 0) count[wave] = __popcll(ballot);
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int i = 0; i < WAVES; ++i) {
-            before += i < wave ? count[i] : 0;
-            all += count[i];
+    for (int r0 = 0; r0 < n_rel; r0 += kScan * kManyThreads) {
+        int c[kScan];
+        uint64_t ballot[kScan];
+#pragma unroll
+        for (int u = 0; u < kScan; ++u) {
+            const int r = r0 + u * kManyThreads + tid;
+            c[u] = r < n_rel ? a.of[r] : -1;
         }
-        if (in) {
-            const int at = before + __popcll(ballot & ((1ull << lane) - 1));
-            list[at] = r0 + tid;
-            of[at] = c - c0;
+#pragma unroll
+        for (int u = 0; u < kScan; ++u) {
+            ballot[u] = __ballot(c[u] >= c0 && c[u] < c1);
+            if (lane == 0) count[u * WAVES + wave] = __popcll(ballot[u]);
+        }
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int u = 0; u < kScan; ++u) {
+            int at = all + __popcll(ballot[u] & ((1ull << lane) - 1));
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                const int n = count[u * WAVES + i];
+                at += i < wave ? n : 0;
+                all += n;
+            }
+            if (c[u] >= c0 && c[u] < c1) {
+                list[at] = r0 + u * kManyThreads + tid;
+                of[at] = static_cast<uint8_t>(c[u] - c0);
+            }
         }
         __syncthreads();
         for (int e0 = 0; e0 < all; e0 += 16) {
@@ -953,6 +970,9 @@ static hipError_t by_length(const RelArgs &a, const RelPlan &p, hipStream_t st)
             case 16 * 16 + 1: return run(k_rel_rows<T, 16, 1, BACK>, a, p, BACK, st);
             case 32 * 16 + 1: return run(k_rel_rows<T, 32, 1, BACK>, a, p, BACK, st);
             case 32 * 16 + 2: return run(k_rel_rows<T, 32, 2, BACK>, a, p, BACK, st);
+            case 32 * 16 + 3:
+                if constexpr (!BACK && sizeof(T) == 2) return run(k_rel_rows<T, 32, 3, BACK>, a, p, BACK, st);
+                [[fallthrough]];                          // none with these
             default: return run(k_rel_rows<T, 64, 2, BACK>, a, p, BACK, st);
         }
     }
