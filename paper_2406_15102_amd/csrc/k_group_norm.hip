@@ -23,6 +23,7 @@ struct GroupNormPlan {
     int ve, lanes, threads, rows, slabs, chunks, nv;
     int chunk_px;                // positions of a chunk, a multiple of `rows`
     bool whole;
+    bool near;                   // the slabs of a chunk side by side on one XCD
     bool aligned;                // lanes a power of two up to 64: lanes of a wavefront that are congruent modulo it have the same channels
 };
 
@@ -77,11 +78,11 @@ GroupNormPlan plan_for(int64_t Nb, int64_t P, int C, int cg, bool is_f32, bool b
         }
     }
     if (p.whole) return p;
-    // Chunks: enough workgroups to fill the chip once (four to a compute unit; twice as many took 123 us for 16 x 96 x 96 x 320 backward where this
-    // takes 111), at most 256 a slab, for every workgroup of the second launch folds them.
+    // Chunks: enough workgroups to fill the chip once (four to a compute unit, and none that would be a fifth: 30 x 67 x 68 x 128 backward 55 us by
+    // 1080 workgroups and 47 by 1020; twice as many took 123 us for 16 x 96 x 96 x 320 backward where this takes 111), at most 256 a slab, for every workgroup of the second launch folds them.
     p.threads = p.lanes > 256 ? 1024 : 256;
     p.rows = p.threads / p.lanes;
-    int64_t chunks = (1024 + pairs - 1) / pairs;
+    int64_t chunks = 1024 / pairs;
     // Four positions to a thread at least, so that what a workgroup spends before and after is worth it; two where few workgroups would be there
     // and few sums to fold (22 x 41 x 42 x 16 backward: 17.3 us with four, 14.7 with two; 64 x 32 x 32 x 64, 512 workgroups: 20.2 and 25.4;
     // 2 x 77 x 78 x 96, 72 chunks: 18.4 and 21.1).
@@ -93,6 +94,9 @@ GroupNormPlan plan_for(int64_t Nb, int64_t P, int C, int cg, bool is_f32, bool b
     const int64_t px = ((P + chunks - 1) / chunks + p.rows - 1) / p.rows * p.rows;
     p.chunk_px = static_cast<int>(px);
     p.chunks = static_cast<int>((P + px - 1) / px);
+    // Where slabs share lines, those of a chunk run one after the other on one XCD, whose L2 then reads and writes a line once (28 x 73 x 73 x 180 in
+    // fp32, 144 bytes a slab, backward 106 us, else 143); with whole lines there is nothing to share (12 x 93 x 94 x 256 in fp32: 115 and 103).
+    p.near = slab * (is_f32 ? 4 : 2) % kSlabBytes != 0 && p.slabs > 1 && Nb * p.chunks >= 64;
     return p;
 }
 
@@ -103,7 +107,10 @@ struct Spot {
     int lane, row, rows, ncol, c0, c, ng;      // ncol: channels of a slab; c: first channel of the thread; ng: groups of the slab
     int img, slab, chunk;
     bool on;
+    bool idle;                                 // the workgroup has no slab
 };
+// CHUNKS: of a map in chunks
+template <bool CHUNKS>
 __device__ __forceinline__ Spot spot_of(const GroupNormArgs &a, const GroupNormPlan &p, int ve, int block)
 {
     Spot s;
@@ -111,10 +118,19 @@ __device__ __forceinline__ Spot spot_of(const GroupNormArgs &a, const GroupNormP
     s.lane = static_cast<int>(threadIdx.x) - s.row * p.lanes;
     s.rows = p.rows;
     s.ncol = p.lanes * ve;
-    const int pair = block / p.chunks;
-    s.chunk = block - pair * p.chunks;
-    s.img = pair / p.slabs;
-    s.slab = pair - s.img * p.slabs;
+    if (CHUNKS && p.near) {                    // workgroups go round the eight XCDs: every eighth has the next slab of a chunk
+        const int of = (block >> 3) / p.slabs, unit = of * 8 + (block & 7);
+        s.slab = (block >> 3) - of * p.slabs;
+        s.img = unit / p.chunks;
+        s.chunk = unit - s.img * p.chunks;
+        s.idle = s.img >= a.Nb;
+    } else {
+        const int pair = block / p.chunks;
+        s.chunk = block - pair * p.chunks;
+        s.img = pair / p.slabs;
+        s.slab = pair - s.img * p.slabs;
+        s.idle = false;
+    }
     s.c0 = s.slab * s.ncol;
     s.c = s.c0 + s.lane * ve;
     const int nch = a.C - s.c0 < s.ncol ? a.C - s.c0 : s.ncol;
@@ -285,7 +301,7 @@ template <typename T, int VE, int NV, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_gn_tile(GroupNormArgs a, GroupNormPlan p)
 {
     extern __shared__ float lds[];
-    const Spot s = spot_of(a, p, VE, blockIdx.x);
+    const Spot s = spot_of<false>(a, p, VE, blockIdx.x);
     const Sums m = sums_of(lds, p, s.ncol);
     const Places l = places_at<T, VE>(a, s, 0, a.P);
     const int left = static_cast<int>(a.P) - s.row;             // positions from the thread's first to the end, `rows` apart
@@ -366,7 +382,8 @@ template <typename T, int VE, int U, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_gn_stats(GroupNormArgs a, GroupNormPlan p)
 {
     extern __shared__ float lds[];
-    const Spot s = spot_of(a, p, VE, blockIdx.x);
+    const Spot s = spot_of<true>(a, p, VE, blockIdx.x);
+    if (s.idle) return;
     const Sums m = sums_of(lds, p, s.ncol);
     const int64_t p0 = static_cast<int64_t>(s.chunk) * p.chunk_px, p1 = p0 + p.chunk_px < a.P ? p0 + p.chunk_px : a.P;
     float n = 0.0f, mean[VE], m2[VE], u[U][VE];
@@ -434,7 +451,8 @@ __global__ __launch_bounds__(THREADS) void k_gn_apply(GroupNormArgs a, GroupNorm
 {
     extern __shared__ float lds[];
     const int64_t bytes = static_cast<int64_t>(a.Nb) * a.P * a.C * static_cast<int64_t>(sizeof(T));
-    const Spot s = spot_of(a, p, VE, reverse_same_xcd(blockIdx.x, gridDim.x, bytes));
+    const Spot s = spot_of<true>(a, p, VE, reverse_same_xcd(blockIdx.x, gridDim.x, bytes));
+    if (s.idle) return;
     const int tid = static_cast<int>(threadIdx.x), T_ = static_cast<int>(blockDim.x);
     const int64_t p0 = static_cast<int64_t>(s.chunk) * p.chunk_px, p1 = p0 + p.chunk_px < a.P ? p0 + p.chunk_px : a.P;
     Raw<T, VE> next[U];
@@ -590,7 +608,7 @@ template <typename T, int VE, int NV, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_gn_grad_tile(GroupNormArgs a, GroupNormPlan p)
 {
     extern __shared__ float lds[];
-    const Spot s = spot_of(a, p, VE, blockIdx.x);
+    const Spot s = spot_of<false>(a, p, VE, blockIdx.x);
     const Sums m = sums_of(lds, p, s.ncol);
     float *chB = m.grp + s.ncol, *gB = chB + s.ncol;
     const Places l = places_at<T, VE>(a, s, 0, a.P);
@@ -670,7 +688,8 @@ template <typename T, int VE, int U, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_gn_grad_sums(GroupNormArgs a, GroupNormPlan p)
 {
     extern __shared__ float lds[];
-    const Spot s = spot_of(a, p, VE, blockIdx.x);
+    const Spot s = spot_of<true>(a, p, VE, blockIdx.x);
+    if (s.idle) return;
     const Sums m = sums_of(lds, p, s.ncol);
     float *chB = m.grp + s.ncol;
     const int64_t p0 = static_cast<int64_t>(s.chunk) * p.chunk_px, p1 = p0 + p.chunk_px < a.P ? p0 + p.chunk_px : a.P;
@@ -751,7 +770,8 @@ __global__ __launch_bounds__(THREADS) void k_gn_grad_apply(GroupNormArgs a, Grou
         return;
     }
     const int64_t bytes = 2 * static_cast<int64_t>(a.Nb) * a.P * a.C * static_cast<int64_t>(sizeof(T));
-    const Spot s = spot_of(a, p, VE, reverse_same_xcd(blockIdx.x - side, gridDim.x - side, bytes));
+    const Spot s = spot_of<true>(a, p, VE, reverse_same_xcd(blockIdx.x - side, gridDim.x - side, bytes));
+    if (s.idle) return;
     const int tid = static_cast<int>(threadIdx.x), T_ = static_cast<int>(blockDim.x);
     const int64_t p0 = static_cast<int64_t>(s.chunk) * p.chunk_px, p1 = p0 + p.chunk_px < a.P ? p0 + p.chunk_px : a.P;
     GradStream<T, VE, U> in;
@@ -824,13 +844,19 @@ size_t group_norm_ws_bytes(int64_t Nb, int64_t P, int C, int groups, bool is_f32
 template <typename T, int VE, bool LONG> constexpr int stream_vectors() { return VE == 8 ? (LONG ? 4 : 2) / (sizeof(T) == 2 ? 1 : 2) : 4; }
 static bool long_chunks(const GroupNormPlan &p) { return p.chunk_px >= 16 * p.rows; }
 
+static unsigned blocks_of(const GroupNormArgs &a, const GroupNormPlan &p)
+{
+    const int64_t units = static_cast<int64_t>(a.Nb) * p.chunks;
+    return static_cast<unsigned>((p.near ? (units + 7) / 8 * 8 : units) * p.slabs);
+}
+
 // THREADS: the most that the kernels are compiled for -- a larger workgroup has fewer registers to a thread
 template <typename T, int VE, int THREADS>
 static hipError_t forward(const GroupNormArgs &a, const GroupNormPlan &p, hipStream_t st)
 {
     constexpr int U = stream_vectors<T, VE, false>(), UL = stream_vectors<T, VE, true>();
     const bool far = long_chunks(p);
-    const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.Nb) * p.slabs * p.chunks);
+    const unsigned blocks = blocks_of(a, p);
     const size_t lds = sums_lds_bytes(p);
     if (p.whole) {
         if (p.nv == 16 / VE) k_gn_tile<T, VE, 16 / VE, THREADS><<<blocks, p.threads, lds, st>>>(a, p);
@@ -850,17 +876,18 @@ static hipError_t backward(const GroupNormArgs &a, const GroupNormPlan &p, hipSt
 {
     constexpr int U = stream_vectors<T, VE, false>(), UL = stream_vectors<T, VE, true>();
     const bool far = long_chunks(p);
-    const unsigned blocks = static_cast<unsigned>(static_cast<int64_t>(a.Nb) * p.slabs * p.chunks);
+    const unsigned blocks = blocks_of(a, p);
     const size_t ncol = static_cast<size_t>(p.lanes) * VE, lds = sums_lds_bytes(p) + 2 * ncol * sizeof(float);
     const bool params = a.dw || a.db;
-    const int side = params ? (a.C + 15) / 16 : 0;
+    // a multiple of 8, so that the second launch's workgroups find their chunks in the L2s that read them
+    const int side = params ? ((a.C + 15) / 16 + 7) / 8 * 8 : 0;
     if (p.whole) {
         if (blocks) {
             if (p.nv == 16 / VE) k_gn_grad_tile<T, VE, 16 / VE, THREADS><<<blocks, p.threads, lds, st>>>(a, p);
             else k_gn_grad_tile<T, VE, 32 / VE, THREADS><<<blocks, p.threads, lds, st>>>(a, p);
             if (const hipError_t e = hipGetLastError()) return e;
         }
-        if (params) k_gn_param_grads<<<side, 1024, 2 * 1024 * sizeof(float), st>>>(a, a.Nb);
+        if (params) k_gn_param_grads<<<(a.C + 15) / 16, 1024, 2 * 1024 * sizeof(float), st>>>(a, a.Nb);
         return hipGetLastError();
     }
     if (blocks && far) k_gn_grad_sums<T, VE, UL, THREADS><<<blocks, p.threads, lds, st>>>(a, p);
