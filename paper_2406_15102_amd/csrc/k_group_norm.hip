@@ -11,8 +11,8 @@
 // means and squared distances from them (no difference of large sums anywhere), and a second launch reads x again, from the last-level
 // cache where the tensor fits it.
 // Measured: 64 x 14 x 14 x 256 in bf16 with ReLU, forward, 7.5 us, of which a launch's own time is half; 512 of them 25.2 us (4.1 TB/s).
-// 16 x 96 x 96 x 320 in bf16 with SiLU, backward: 111 us; the sums read x and dy in 41 us (4.6 TB/s), the second launch reads them again and writes dx in 57
-// (5.2 TB/s), so of what a second reading leaves (92 us at the rate of a large copy) 17 % is lost.  Vector instructions alone: 22 and 23 us.
+// 16 x 96 x 96 x 320 in bf16 with SiLU, backward: 112 us; the sums read x and dy in 41 us (4.6 TB/s), the second launch reads them again and writes dx in 56
+// (5.1 TB/s); the bytes of both readings take 92 us at the rate of a large copy.  Vector instructions alone: 22 and 23 us.
 // Statistics and sums are fp32; the order of every sum is fixed by the shape, so results repeat bit for bit.
 #include "around_device.hpp"
 
@@ -79,7 +79,7 @@ GroupNormPlan plan_for(int64_t Nb, int64_t P, int C, int cg, bool is_f32, bool b
     }
     if (p.whole) return p;
     // Chunks: enough workgroups to fill the chip once (four to a compute unit, and none that would be a fifth: 30 x 67 x 68 x 128 backward 55 us by
-    // 1080 workgroups and 47 by 1020; twice as many took 123 us for 16 x 96 x 96 x 320 backward where this takes 111), at most 256 a slab, for every workgroup of the second launch folds them.
+    // 1080 workgroups and 47 by 1020; twice as many took 123 us for 16 x 96 x 96 x 320 backward where this takes 112), at most 256 a slab, for every workgroup of the second launch folds them.
     p.threads = p.lanes > 256 ? 1024 : 256;
     p.rows = p.threads / p.lanes;
     int64_t chunks = 1024 / pairs;
@@ -879,7 +879,8 @@ static hipError_t backward(const GroupNormArgs &a, const GroupNormPlan &p, hipSt
     const unsigned blocks = blocks_of(a, p);
     const size_t ncol = static_cast<size_t>(p.lanes) * VE, lds = sums_lds_bytes(p) + 2 * ncol * sizeof(float);
     const bool params = a.dw || a.db;
-    // a multiple of 8, so that the second launch's workgroups find their chunks in the L2s that read them
+    // A multiple of 8, so that a chunk's workgroup of the second launch is on the XCD of its first one's: 17 x 30 x 31 x 192 in fp32 20.4 us, else
+    // 22.5 (the bytes that the L2s fetch are the same either way).
     const int side = params ? ((a.C + 15) / 16 + 7) / 8 * 8 : 0;
     if (p.whole) {
         if (blocks) {
