@@ -117,6 +117,13 @@ def test_maps_in_chunks(Nb, P, C, groups, dtype):
     _compare(x, w, b, dy, groups, 2, 0.1, 3, _run(x, w, b, dy, groups, 2, 0.1, 3))
 
 
+@pytest.mark.parametrize("Nb,P,C,groups,dtype", [(9, 1640, 180, 15, F32), (7, 2500, 320, 32, BF16), (17, 930, 192, 32, F32), (64, 1500, 80, 8, F32)])
+def test_slabs_that_share_lines(Nb, P, C, groups, dtype):
+    """Several slabs whose bytes are no whole lines, chunks whose number is a multiple of 8 and chunks whose number is not."""
+    x, w, b, dy = _inputs(Nb, P, C, dtype, F32, P)
+    _compare(x, w, b, dy, groups, 3, 0.1, 3, _run(x, w, b, dy, groups, 3, 0.1, 3))
+
+
 @pytest.mark.parametrize("P", [60, 6000])
 @pytest.mark.parametrize("first", [0.0, 1000.0, 1e6])
 def test_far_off_zero(P, first):
